@@ -104,6 +104,84 @@ int specext_verify_attn(const specext_attn_desc* desc, const void* Q, const void
                         void* cuda_stream);
 
 /*
+ * The prefix cache in 8 bits.  A cached value is code * 2^(scale - 127): one e4m3 code per value, and one
+ * e8m0 scale (a byte: the exponent of a power of two, 255 = NaN) for each block of block_tokens tokens and
+ * KV head, for K and for V.  Against bf16 it is half the memory and half the bytes of a decoding step.  Codes
+ * are laid out like the bf16 cache, strides in bytes (multiples of 16); token t's scales are those of block
+ * t / block_tokens.
+ */
+typedef struct {
+  int32_t block_tokens;                    /* B: 32, 64 or 128 (UNSUPPORTED otherwise)         */
+  int32_t reserved;                        /* 0                                                */
+  int64_t scale_stride_b, scale_stride_h;  /* K_scale and V_scale [>=ceil(L/B)][Hkv], in bytes */
+} specext_q8_desc;
+
+/*
+ * Appends tokens to the 8-bit cache: token i of n_tokens goes to position start + i.
+ *
+ *   K, V     : bf16 [n_src][n_kv_heads][head_dim], strides in elements (multiples of 8); head_dim 64 or 128.
+ *   rows     : int32 [n_tokens] in device memory, the row of K and V that each token is taken from (the
+ *              accepted nodes of a draft tree, say; a row may come twice), or NULL: token i is row i.  A row outside
+ *              [0, n_src) becomes zeros and is reported as INVALID_ARG in *device_status.
+ *   K_codes, V_codes : [>= start + n_tokens][n_kv_heads][head_dim];  K_scale, V_scale as in q8.
+ * The scale of a block is the smallest power of two s, at least 2^-100, with |x| <= 448 s for its new tokens;
+ * codes are round-to-nearest-even of x / s.  The block that `start` falls into the middle of holds earlier tokens:
+ * its scale stays or grows to what the new ones need, and where it grows the earlier codes are divided by the
+ * power of two (which rounds those that become subnormal).  A NaN or infinity among the new tokens makes
+ * the scale of its block NaN (codes are not written then), and so it stays while tokens are appended to the
+ * block: attention over it is NaN.
+ * Codes behind start + n_tokens and scales of other blocks are left as they are.  Start at a block's
+ * first token to give it a scale anew.  K and V must not overlap the codes.
+ */
+int specext_quantize_kv(const void* K, const void* V, int32_t n_src, int32_t n_kv_heads, int32_t head_dim,
+                        int64_t stride_l, int64_t stride_h, const int32_t* rows, int32_t n_tokens,
+                        int32_t start, void* K_codes, void* V_codes, int64_t code_stride_l,
+                        int64_t code_stride_h, void* K_scale, void* V_scale, const specext_q8_desc* q8,
+                        int32_t* device_status, void* cuda_stream);
+
+/*
+ * specext_verify_attn with the prefix in an 8-bit cache; n_tree = 1 is single-token decoding.  desc->kv_stride_*
+ * are those of K_codes and V_codes, in bytes and multiples of 16; the tree's keys and values are bf16.  Codes and scales
+ * at and behind prefix_len are never used; the codes 0x7F and 0xFF (NaN), which specext_quantize_kv does not write
+ * to a block with a finite scale, are NaN.
+ * Arithmetic: the result is that of attention on the values the cache stands for.  Codes are multiplied
+ * as f16 (exact), queries and tree keys and values as f16 with a power of two per row or 32 nodes (exact but for values
+ * 2^-28 and more below the largest); products are accumulated in fp32; probabilities, times the V scale, are rounded to f16 for
+ * the product with V (11 bits; 2^-30 and less of a row's largest counts as zero); chunk sums and the normaliser are accumulated in
+ * fp32 from unrounded exponentials.  Everything else as in specext_verify_attn, chunk_score included, so that
+ * SelectChunks and UpdateDraftCache follow unchanged.  The workspace has a size of its own.
+ */
+size_t specext_verify_attn_q8_workspace(const specext_attn_desc* desc, const specext_q8_desc* q8);
+int specext_verify_attn_q8(const specext_attn_desc* desc, const specext_q8_desc* q8, const void* Q,
+                           const void* K_codes, const void* V_codes, const void* K_scale,
+                           const void* V_scale, const void* K_tree, const void* V_tree,
+                           const int32_t* parent, void* O, float* lse, float* chunk_score,
+                           void* workspace, size_t workspace_bytes, int32_t* device_status,
+                           void* cuda_stream);
+
+/*
+ * Log probabilities under rows of logits, as a step needs them on both sides of the verification: of the tokens that
+ * the children of a tree node propose, of the best continuations (tree expansion), and the entropy.  Per row, with
+ * x = logits / temperature:
+ *   lse = log sum_w e^(x_w),  logprob[i] = x[tokens[i]] - lse,  entropy = -sum_w p_w log p_w (nats),
+ *   top_ids / top_logprob: the n_best largest logits in descending order, equal ones by the lower index.
+ *
+ *   logits  : bf16, or fp32 when logits_fp32 != 0, [n_rows][vocab] with row stride stride_row >= vocab (any), any
+ *             alignment of its type; -inf (a masked word) is allowed.  vocab <= 2^30.
+ *   tokens  : int32 [n_rows][n_given]; -1 is "no token" and gets -inf; others outside [0, vocab) get -inf and are
+ *             reported as INVALID_ARG in *device_status.  n_given may be 0.
+ *   logprob : fp32 [n_rows][n_given];  entropy, lse : fp32 [n_rows];
+ *   top_ids : int32, top_logprob : fp32, [n_rows][n_best], 0 <= n_best <= min(32, vocab).
+ * A row without a finite logit (all -inf) has lse = -inf, log probabilities -inf and entropy 0; a row
+ * with a NaN or +inf has NaN everywhere and top_ids -1.  Sums are fp32; the logits are read once.
+ */
+int specext_token_logprobs(const void* logits, int32_t logits_fp32, int32_t n_rows, int32_t vocab,
+                           int64_t stride_row, float temperature, const int32_t* tokens,
+                           int32_t n_given, int32_t n_best, float* logprob, float* entropy, float* lse,
+                           int32_t* top_ids, float* top_logprob, int32_t* device_status,
+                           void* cuda_stream);
+
+/*
  * SelectChunks of Algorithm 1 (Appendix A; Section 3.2.1: rank the fixed-size chunks of the
  * prefix by their average attention score for one query and keep the top k).
  *

@@ -41,9 +41,16 @@ class AttnDesc(ctypes.Structure):
                 ("o_stride_t", ctypes.c_int64), ("o_stride_h", ctypes.c_int64)]
 
 
+class Q8Desc(ctypes.Structure):
+    """Mirror of specext_q8_desc."""
+    _fields_ = [("block_tokens", ctypes.c_int32), ("reserved", ctypes.c_int32), ("scale_stride_b", ctypes.c_int64),
+                ("scale_stride_h", ctypes.c_int64)]
+
+
 _LIB: Optional[ctypes.CDLL] = None
 _BINDING = None
-_ENTRIES = ("verify_attn", "draft_attn", "prefill_attn", "select_gather")     # called through the extension module
+_ENTRIES = ("verify_attn", "draft_attn", "prefill_attn", "select_gather", "verify_attn_q8", "quantize_kv",
+            "token_logprobs")     # called through the extension module
 
 
 def bind(path: str) -> ctypes.CDLL:
@@ -65,6 +72,15 @@ def bind(path: str) -> ctypes.CDLL:
     L.specext_draft_attn.argtypes = [ctypes.POINTER(AttnDesc)] + [vp] * 9 + [vp, sz, vp, vp]
     L.specext_prefill_attn.restype = ctypes.c_int
     L.specext_prefill_attn.argtypes = [ctypes.POINTER(AttnDesc)] + [vp] * 7
+    L.specext_verify_attn_q8_workspace.restype = sz
+    L.specext_verify_attn_q8_workspace.argtypes = [ctypes.POINTER(AttnDesc), ctypes.POINTER(Q8Desc)]
+    L.specext_verify_attn_q8.restype = ctypes.c_int
+    L.specext_verify_attn_q8.argtypes = [ctypes.POINTER(AttnDesc), ctypes.POINTER(Q8Desc)] + [vp] * 12 + [sz, vp, vp]
+    L.specext_quantize_kv.restype = ctypes.c_int
+    L.specext_quantize_kv.argtypes = [vp, vp, i32, i32, i32, i64, i64, vp, i32, i32, vp, vp, i64, i64, vp, vp,
+                                      ctypes.POINTER(Q8Desc), vp, vp]
+    L.specext_token_logprobs.restype = ctypes.c_int
+    L.specext_token_logprobs.argtypes = [vp, i32, i32, i32, i64, ctypes.c_float, vp, i32, i32] + [vp] * 7
     L.specext_select_gather.restype = ctypes.c_int
     L.specext_select_gather.argtypes = [vp, i32, i32, i32, i32, i32, i32, i32, i32, vp, vp, i32, i32, i32, i64, i64,
                                         i64, vp, vp, vp, vp, vp, vp, vp]
@@ -127,7 +143,8 @@ def _check(code: int, where: str) -> None:
 def make_attn_desc(Q: torch.Tensor, K_prefix: torch.Tensor, K_tree: torch.Tensor, O: torch.Tensor,
                    prefix_len: int, chunk_size: int, softmax_scale: float = 0.0,
                    want_chunk_score: bool = False) -> AttnDesc:
-    """Fills a specext_attn_desc from tensor shapes and strides (V tensors share K's strides)."""
+    """Fills a specext_attn_desc from tensor shapes and strides (V tensors share K's strides); K_prefix may be the codes of a
+    cache in 8 bits."""
     d = AttnDesc()
     _binding().fill_desc(d, Q, K_prefix, K_tree, O, int(prefix_len), int(chunk_size), softmax_scale, want_chunk_score)
     return d
@@ -165,6 +182,47 @@ def specext_prefill_attn(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, O: t
     rc = _binding().prefill_attn(lib().entry["prefill_attn"], Q, K, V, O, lse, device_status, softmax_scale)
     if rc:
         raise SpecextError(rc, "specext_prefill_attn")
+
+
+def specext_verify_attn_q8_workspace(desc: AttnDesc, block_tokens: int) -> int:
+    """Bytes of scratch for specext_verify_attn_q8 (0 for a descriptor that it does not take)."""
+    q = Q8Desc(int(block_tokens), 0, 1, 1)                       # (the size does not depend on the strides)
+    return int(lib().specext_verify_attn_q8_workspace(ctypes.byref(desc), ctypes.byref(q)))
+
+
+def specext_verify_attn_q8(desc: AttnDesc, Q: torch.Tensor, K_codes: torch.Tensor, V_codes: torch.Tensor,
+                           K_scale: torch.Tensor, V_scale: torch.Tensor, block_tokens: int, K_tree: torch.Tensor,
+                           V_tree: torch.Tensor, parent: torch.Tensor, O: torch.Tensor, lse: torch.Tensor,
+                           chunk_score: Optional[torch.Tensor], workspace: torch.Tensor,
+                           device_status: torch.Tensor) -> None:
+    """specext_verify_attn over a prefix in 8 bits: codes float8_e4m3fn [>=L][Hkv][D], scales float8_e8m0fnu [>=L/B][Hkv]."""
+    rc = (_BINDING or _binding()).verify_attn_q8((_LIB or lib()).entry["verify_attn_q8"], desc, Q, K_codes, V_codes, K_scale,
+                                                 V_scale, block_tokens, K_tree, V_tree, parent, O, lse, chunk_score, workspace,
+                                                 device_status)
+    if rc:
+        raise SpecextError(rc, "specext_verify_attn_q8")
+
+
+def specext_quantize_kv(K: torch.Tensor, V: torch.Tensor, start: int, K_codes: torch.Tensor, V_codes: torch.Tensor,
+                        K_scale: torch.Tensor, V_scale: torch.Tensor, block_tokens: int, device_status: torch.Tensor,
+                        rows: Optional[torch.Tensor] = None) -> None:
+    """Enqueues the append of tokens to an 8-bit cache at position `start`: all rows of K and V [n][Hkv][D] (bf16), or those
+    that the int32 vector `rows` (on the device) names, in its order."""
+    rc = (_BINDING or _binding()).quantize_kv((_LIB or lib()).entry["quantize_kv"], K, V, start, K_codes, V_codes, K_scale,
+                                              V_scale, block_tokens, device_status, rows)
+    if rc:
+        raise SpecextError(rc, "specext_quantize_kv")
+
+
+def specext_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor], logprob: Optional[torch.Tensor],
+                           entropy: torch.Tensor, lse: torch.Tensor, top_ids: Optional[torch.Tensor],
+                           top_logprob: Optional[torch.Tensor], device_status: torch.Tensor, temperature: float = 1.0) -> None:
+    """Enqueues the log probabilities of given tokens, the entropy and the best words of rows of logits (bf16 or fp32
+    [rows][vocab]).  tokens / logprob [rows][given] and top_ids / top_logprob [rows][best] may be None."""
+    rc = (_BINDING or _binding()).token_logprobs((_LIB or lib()).entry["token_logprobs"], logits, tokens, logprob, entropy, lse,
+                                                 top_ids, top_logprob, device_status, temperature)
+    if rc:
+        raise SpecextError(rc, "specext_token_logprobs")
 
 
 STATIC_SCRATCH_BYTES = 32 << 20

@@ -3,8 +3,15 @@
 #include <cmath>
 #include <cstring>
 
-#include "common.cuh"
+#include "q8.cuh"
 
+cudaError_t spx_launch_quantize(const void* K, const void* V, int n_kv_heads, int head_dim, long long x_sl, long long x_sh,
+                                const int32_t* rows, int n_src, int n, int start, void* Kc, void* Vc, long long c_sl,
+                                long long c_sh, void* Ks, void* Vs, long long s_sb, long long s_sh, int log_block,
+                                int32_t* status, cudaStream_t st);
+cudaError_t spx_launch_logprobs(const void* logits, bool f32, int rows, int V, long long stride, float inv_temperature,
+                                const int32_t* tokens, int given, int best, float* logprob, float* entropy, float* lse,
+                                int32_t* top_ids, float* top_logprob, int n_sm, int32_t* status, cudaStream_t st);
 cudaError_t spx_launch_select(const float* score_row, int NC, int L, int C, int k, int n_sink, int n_recent,
                               int32_t* idx, int32_t* n_selected, cudaStream_t st);
 cudaError_t spx_launch_gather(const void* dK, const void* dV, int n_layers, int H, int D, int L, int C,
@@ -64,6 +71,20 @@ int sm_count() {
 
 bool is_pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+void lay_out_workspace(AttnPlan* plan) {
+  AttnPlan& p = *plan;
+  p.n_slots = p.cluster > 0 ? p.n_cta : p.n_cta + p.NP - 1;
+  long long off = 0;
+  p.off_part_o = off; off += (long long)p.n_slots * p.D * p.RB;
+  p.off_part_m = off; off += (long long)p.n_slots * p.RB;
+  p.off_part_l = off; off += (long long)p.n_slots * p.RB;
+  if (p.want_score) {
+    p.off_mass = off; off += (long long)p.NP * p.TPH * p.RB * p.CPT;
+    p.off_mref = off; off += (long long)p.NP * p.TPH * p.RB;
+  }
+  p.total_floats = off;
+}
 
 // Row blocks, workers and workspace of one kernel (plan.kernel); cluster > 0: its workers merge in clusters of that size.
 int lay_out(AttnPlan* plan, int kernel, int row_block, int cluster) {
@@ -126,16 +147,7 @@ int lay_out(AttnPlan* plan, int kernel, int row_block, int cluster) {
     if (p.cluster > 0 && p.rows <= kSpxClusterRowsBySmem) p.q_rows = 32;       // (the exchange needs the room, see Layout)
     else if (p.rows <= 64 && p.U / p.n_cta < 12) p.q_rows = 64;
   }
-  p.n_slots = p.cluster > 0 ? p.n_cta : p.n_cta + p.NP - 1;
-  long long off = 0;
-  p.off_part_o = off; off += (long long)p.n_slots * p.D * p.RB;
-  p.off_part_m = off; off += (long long)p.n_slots * p.RB;
-  p.off_part_l = off; off += (long long)p.n_slots * p.RB;
-  if (p.want_score) {
-    p.off_mass = off; off += (long long)p.NP * p.TPH * p.RB * p.CPT;
-    p.off_mref = off; off += (long long)p.NP * p.TPH * p.RB;
-  }
-  p.total_floats = off;
+  lay_out_workspace(plan);
   return SPECEXT_OK;
 }
 
@@ -216,8 +228,8 @@ int cluster_size(const AttnPlan& p, bool pair, bool dev_len) {
   return size;
 }
 
-// (The workspace is that of the split form whatever dev_len is: the clusters' is never larger.)
-int build_plan(const specext_attn_desc* d, AttnPlan* out, bool dev_len = false) {
+// Checks of the descriptor, and the sizes that do not depend on the kernel.
+int plan_sizes(const specext_attn_desc* d, AttnPlan* out) {
   if (!d) return SPECEXT_ERR_INVALID_ARG;
   if (d->n_q_heads < 1 || d->n_kv_heads < 1 || d->n_q_heads % d->n_kv_heads != 0) return SPECEXT_ERR_INVALID_ARG;
   if (d->prefix_len < 0 || d->prefix_len > (1 << 24)) return SPECEXT_ERR_INVALID_ARG;
@@ -244,11 +256,20 @@ int build_plan(const specext_attn_desc* d, AttnPlan* out, bool dev_len = false) 
   p.want_score = d->want_chunk_score != 0;
   const float scale = d->softmax_scale > 0.f ? d->softmax_scale : 1.0f / std::sqrt((float)p.D);
   p.scale2 = scale * 1.44269504088896340736f;
+  *out = p;
+  return SPECEXT_OK;
+}
+
+// (The workspace is that of the split form whatever dev_len is: the clusters' is never larger.)
+int build_plan(const specext_attn_desc* d, AttnPlan* out, bool dev_len = false) {
+  AttnPlan p;
+  int rc = plan_sizes(d, &p);
+  if (rc != SPECEXT_OK) return rc;
   // Kernel: pairs of CTAs on 256-row blocks for head_dim 128 and more than 128 stacked rows; otherwise one CTA on
   // 128-row blocks (want != 0 only in the test library).
   const int want = tuning_kernel();
   const bool pair = p.D == 128 && p.rows > 128 && want != 2;
-  int rc = lay_out(&p, want == 1 ? 1 : (pair ? 3 : 2), pair ? 256 : 128, 0);
+  rc = lay_out(&p, want == 1 ? 1 : (pair ? 3 : 2), pair ? 256 : 128, 0);
   if (rc != SPECEXT_OK) return rc;
   const int size = want == 0 && tuning_min_units() == 1 ? cluster_size(p, pair, dev_len) : 0;
   if (size > 0) {
@@ -258,6 +279,37 @@ int build_plan(const specext_attn_desc* d, AttnPlan* out, bool dev_len = false) 
     if (rc != SPECEXT_OK) return rc;
     if (p.total_floats < split_floats) p.total_floats = split_floats;
   }
+  *out = p;
+  return SPECEXT_OK;
+}
+
+// Whether 8-bit tensors with these strides can be copied in 16-byte pieces.
+bool q8_strides(long long a, long long b, int head_dim) { return a >= head_dim && b >= head_dim && ((a | b) & 15) == 0; }
+int block_log2(int block_tokens) { return block_tokens == 32 ? 5 : block_tokens == 64 ? 6 : block_tokens == 128 ? 7 : 0; }
+
+// The plan of an attention call on the 8-bit cache: every problem has the same whole number of workers.
+int build_plan_q8(const specext_attn_desc* d, const specext_q8_desc* q, AttnPlan* out) {
+  AttnPlan p;
+  const int rc = plan_sizes(d, &p);
+  if (rc != SPECEXT_OK) return rc;
+  if (!q || block_log2(q->block_tokens) == 0) return q ? SPECEXT_ERR_UNSUPPORTED : SPECEXT_ERR_INVALID_ARG;
+  if (!q8_strides(d->kv_stride_l, d->kv_stride_h, d->head_dim) || q->scale_stride_b < 1 || q->scale_stride_h < 1)
+    return SPECEXT_ERR_INVALID_ARG;
+  p.kernel = 4;
+  p.RB = p.q_rows = 128;
+  p.n_rblk = (p.rows + p.RB - 1) / p.RB;
+  const long long np = (long long)p.Hkv * p.n_rblk;
+  if (np * p.UPP > (1ll << 30)) return SPECEXT_ERR_UNSUPPORTED;
+  p.NP = (int)np;
+  p.U = p.NP * p.UPP;
+  p.cpp = sm_count() / p.NP;
+  if (p.cpp > p.UPP) p.cpp = p.UPP;
+  if (p.cpp < 1) p.cpp = 1;
+  p.n_cta = p.NP * p.cpp;
+  p.q = p.UPP / p.cpp;
+  p.rem = p.UPP % p.cpp;
+  p.max_segs = p.cpp;
+  lay_out_workspace(&p);
   *out = p;
   return SPECEXT_OK;
 }
@@ -293,6 +345,38 @@ size_t specext_verify_attn_workspace(const specext_attn_desc* desc) {
 
 namespace {
 
+// The checks of pointers that every attention call makes.
+int check_attn_args(const AttnPlan& p, const void* Q, const void* K_prefix, const void* V_prefix, const void* K_tree,
+                    const void* V_tree, const int32_t* parent, const void* O, const float* lse, const float* chunk_score,
+                    const void* workspace, size_t workspace_bytes) {
+  if (!Q || !K_tree || !V_tree || !parent || !O || !lse || !workspace) return SPECEXT_ERR_INVALID_ARG;
+  if (p.L > 0 && (!K_prefix || !V_prefix)) return SPECEXT_ERR_INVALID_ARG;
+  if (p.want_score && p.NC > 0 && !chunk_score) return SPECEXT_ERR_INVALID_ARG;
+  if (!aligned16(Q) || !aligned16(K_prefix) || !aligned16(V_prefix) || !aligned16(K_tree) ||
+      !aligned16(V_tree) || !aligned16(O) || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 ||
+      (reinterpret_cast<uintptr_t>(lse) & 3u) != 0 || (reinterpret_cast<uintptr_t>(parent) & 3u) != 0)
+    return SPECEXT_ERR_INVALID_ARG;
+  return workspace_bytes < (size_t)p.total_floats * sizeof(float) ? SPECEXT_ERR_WORKSPACE : SPECEXT_OK;
+}
+// Everything but the plan and the prefix.
+void fill_attn_args(AttnArgs* args, const specext_attn_desc* desc, const void* Q, const void* K_tree, const void* V_tree,
+                    const int32_t* parent, void* O, float* lse, float* chunk_score, void* workspace, int32_t* device_status) {
+  AttnArgs& a = *args;
+  a.Q = static_cast<const __nv_bfloat16*>(Q);
+  a.Kt = static_cast<const __nv_bfloat16*>(K_tree);
+  a.Vt = static_cast<const __nv_bfloat16*>(V_tree);
+  a.parent = parent;
+  a.O = static_cast<__nv_bfloat16*>(O);
+  a.lse = lse;
+  a.chunk_score = chunk_score;
+  a.ws = static_cast<float*>(workspace);
+  a.status = device_status;
+  a.q_st = desc->q_stride_t; a.q_sh = desc->q_stride_h;
+  a.kv_sl = desc->kv_stride_l; a.kv_sh = desc->kv_stride_h;
+  a.tkv_st = desc->tkv_stride_t; a.tkv_sh = desc->tkv_stride_h;
+  a.o_st = desc->o_stride_t; a.o_sh = desc->o_stride_h;
+}
+
 // Checks, plan and launches shared by specext_verify_attn (prefix_len_dev == null) and
 // specext_draft_attn (the prefix length is read on the device, desc->prefix_len is its upper bound).
 int run_attn(const specext_attn_desc* desc, const void* Q, const void* K_prefix, const void* V_prefix,
@@ -306,30 +390,11 @@ int run_attn(const specext_attn_desc* desc, const void* Q, const void* K_prefix,
   if (prefix_len_dev && (p.want_score || p.kernel == 1 || (reinterpret_cast<uintptr_t>(prefix_len_dev) & 3u) != 0))
     return p.want_score ? SPECEXT_ERR_INVALID_ARG : (p.kernel == 1 ? SPECEXT_ERR_UNSUPPORTED : SPECEXT_ERR_INVALID_ARG);
   a.L_dev = prefix_len_dev;
-  if (!Q || !K_tree || !V_tree || !parent || !O || !lse || !workspace) return SPECEXT_ERR_INVALID_ARG;
-  if (p.L > 0 && (!K_prefix || !V_prefix)) return SPECEXT_ERR_INVALID_ARG;
-  if (p.want_score && p.NC > 0 && !chunk_score) return SPECEXT_ERR_INVALID_ARG;
-  if (!aligned16(Q) || !aligned16(K_prefix) || !aligned16(V_prefix) || !aligned16(K_tree) ||
-      !aligned16(V_tree) || !aligned16(O) || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 ||
-      (reinterpret_cast<uintptr_t>(lse) & 3u) != 0 || (reinterpret_cast<uintptr_t>(parent) & 3u) != 0)
-    return SPECEXT_ERR_INVALID_ARG;
-  if (workspace_bytes < (size_t)p.total_floats * sizeof(float)) return SPECEXT_ERR_WORKSPACE;
-
-  a.Q = static_cast<const __nv_bfloat16*>(Q);
+  const int bad = check_attn_args(p, Q, K_prefix, V_prefix, K_tree, V_tree, parent, O, lse, chunk_score, workspace, workspace_bytes);
+  if (bad != SPECEXT_OK) return bad;
+  fill_attn_args(&a, desc, Q, K_tree, V_tree, parent, O, lse, chunk_score, workspace, device_status);
   a.Kp = static_cast<const __nv_bfloat16*>(K_prefix);
   a.Vp = static_cast<const __nv_bfloat16*>(V_prefix);
-  a.Kt = static_cast<const __nv_bfloat16*>(K_tree);
-  a.Vt = static_cast<const __nv_bfloat16*>(V_tree);
-  a.parent = parent;
-  a.O = static_cast<__nv_bfloat16*>(O);
-  a.lse = lse;
-  a.chunk_score = chunk_score;
-  a.ws = static_cast<float*>(workspace);
-  a.status = device_status;
-  a.q_st = desc->q_stride_t; a.q_sh = desc->q_stride_h;
-  a.kv_sl = desc->kv_stride_l; a.kv_sh = desc->kv_stride_h;
-  a.tkv_st = desc->tkv_stride_t; a.tkv_sh = desc->tkv_stride_h;
-  a.o_st = desc->o_stride_t; a.o_sh = desc->o_stride_h;
 
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   int n = 0;
@@ -358,6 +423,102 @@ int specext_verify_attn(const specext_attn_desc* desc, const void* Q, const void
                         void* cuda_stream) {
   return run_attn(desc, Q, K_prefix, V_prefix, K_tree, V_tree, parent, nullptr, O, lse, chunk_score, workspace,
                   workspace_bytes, device_status, cuda_stream);
+}
+
+size_t specext_verify_attn_q8_workspace(const specext_attn_desc* desc, const specext_q8_desc* q8) {
+  AttnPlan p;
+  if (build_plan_q8(desc, q8, &p) != SPECEXT_OK) return 0;
+  return (size_t)p.total_floats * sizeof(float);
+}
+
+int specext_verify_attn_q8(const specext_attn_desc* desc, const specext_q8_desc* q8, const void* Q, const void* K_codes,
+                           const void* V_codes, const void* K_scale, const void* V_scale, const void* K_tree,
+                           const void* V_tree, const int32_t* parent, void* O, float* lse, float* chunk_score,
+                           void* workspace, size_t workspace_bytes, int32_t* device_status, void* cuda_stream) {
+  Q8Args q;
+  const int rc = build_plan_q8(desc, q8, &q.a.plan);
+  if (rc != SPECEXT_OK) return rc;
+  AttnArgs& a = q.a;
+  const AttnPlan& p = a.plan;
+  const int bad = check_attn_args(p, Q, K_codes, V_codes, K_tree, V_tree, parent, O, lse, chunk_score, workspace, workspace_bytes);
+  if (bad != SPECEXT_OK) return bad;
+  if (p.L > 0 && (!K_scale || !V_scale)) return SPECEXT_ERR_INVALID_ARG;
+  fill_attn_args(&a, desc, Q, K_tree, V_tree, parent, O, lse, chunk_score, workspace, device_status);
+  a.Kp = a.Vp = nullptr;
+  a.L_dev = nullptr;
+  q.Kc = static_cast<const uint8_t*>(K_codes);
+  q.Vc = static_cast<const uint8_t*>(V_codes);
+  q.Ks = static_cast<const uint8_t*>(K_scale);
+  q.Vs = static_cast<const uint8_t*>(V_scale);
+  q.s_sb = q8->scale_stride_b;
+  q.s_sh = q8->scale_stride_h;
+  q.log_block = block_log2(q8->block_tokens);
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  int n = 0;
+  cudaError_t e = spx_launch_verify_q8(q, st, &n);
+  if (e == cudaSuccess) e = spx_launch_merge(a, st, &n);
+  g_launches.fetch_add(n);
+  if (e != cudaSuccess) {
+    (void)cudaGetLastError();
+    return SPECEXT_ERR_CUDA;
+  }
+  return SPECEXT_OK;
+}
+
+int specext_quantize_kv(const void* K, const void* V, int32_t n_src, int32_t n_kv_heads, int32_t head_dim, int64_t stride_l,
+                        int64_t stride_h, const int32_t* rows, int32_t n_tokens, int32_t start, void* K_codes, void* V_codes,
+                        int64_t code_stride_l, int64_t code_stride_h, void* K_scale, void* V_scale, const specext_q8_desc* q8,
+                        int32_t* device_status, void* cuda_stream) {
+  if (!q8 || !K_codes || !V_codes || !K_scale || !V_scale) return SPECEXT_ERR_INVALID_ARG;
+  if (n_kv_heads < 1 || n_src < 0 || n_tokens < 0 || start < 0 || (long long)start + n_tokens > (1 << 24) ||
+      (!rows && n_tokens > n_src))
+    return SPECEXT_ERR_INVALID_ARG;
+  if (n_tokens > 0 && n_src > 0 && (!K || !V)) return SPECEXT_ERR_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128) return SPECEXT_ERR_UNSUPPORTED;
+  const int log_block = block_log2(q8->block_tokens);
+  if (log_block == 0) return SPECEXT_ERR_UNSUPPORTED;
+  if (stride_l < head_dim || stride_h < head_dim || ((stride_l | stride_h) & 7) != 0 ||
+      !q8_strides(code_stride_l, code_stride_h, head_dim) || q8->scale_stride_b < 1 || q8->scale_stride_h < 1)
+    return SPECEXT_ERR_INVALID_ARG;
+  if (!aligned16(K) || !aligned16(V) || !aligned16(K_codes) || !aligned16(V_codes) || (reinterpret_cast<uintptr_t>(rows) & 3u) != 0)
+    return SPECEXT_ERR_INVALID_ARG;
+  if (n_tokens == 0) return SPECEXT_OK;
+  const long long blocks = ((start + n_tokens - 1) >> log_block) - (start >> log_block) + 1;
+  if (blocks * n_kv_heads > (1ll << 30)) return SPECEXT_ERR_UNSUPPORTED;
+  const cudaError_t e = spx_launch_quantize(K, V, n_kv_heads, head_dim, stride_l, stride_h, rows, n_src, n_tokens, start, K_codes,
+                                            V_codes, code_stride_l, code_stride_h, K_scale, V_scale, q8->scale_stride_b,
+                                            q8->scale_stride_h, log_block, device_status, static_cast<cudaStream_t>(cuda_stream));
+  g_launches.fetch_add(1);
+  if (e != cudaSuccess) {
+    (void)cudaGetLastError();
+    return SPECEXT_ERR_CUDA;
+  }
+  return SPECEXT_OK;
+}
+
+int specext_token_logprobs(const void* logits, int32_t logits_fp32, int32_t n_rows, int32_t vocab, int64_t stride_row,
+                           float temperature, const int32_t* tokens, int32_t n_given, int32_t n_best, float* logprob,
+                           float* entropy, float* lse, int32_t* top_ids, float* top_logprob, int32_t* device_status,
+                           void* cuda_stream) {
+  if (n_rows < 0 || vocab < 1 || n_given < 0 || n_best < 0 || n_best > vocab || stride_row < vocab) return SPECEXT_ERR_INVALID_ARG;
+  if (vocab > (1 << 30) || n_best > 32 || (long long)n_rows > (1ll << 27)) return SPECEXT_ERR_UNSUPPORTED;
+  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.f / temperature)) return SPECEXT_ERR_INVALID_ARG;
+  if (n_rows == 0) return SPECEXT_OK;
+  if (!logits || !entropy || !lse || (n_given > 0 && (!tokens || !logprob)) || (n_best > 0 && (!top_ids || !top_logprob)))
+    return SPECEXT_ERR_INVALID_ARG;
+  const uintptr_t words = reinterpret_cast<uintptr_t>(tokens) | reinterpret_cast<uintptr_t>(logprob) |
+                          reinterpret_cast<uintptr_t>(entropy) | reinterpret_cast<uintptr_t>(lse) |
+                          reinterpret_cast<uintptr_t>(top_ids) | reinterpret_cast<uintptr_t>(top_logprob);
+  if ((words & 3u) != 0 || (reinterpret_cast<uintptr_t>(logits) & (logits_fp32 ? 3u : 1u)) != 0) return SPECEXT_ERR_INVALID_ARG;
+  const cudaError_t e = spx_launch_logprobs(logits, logits_fp32 != 0, n_rows, vocab, stride_row, 1.f / temperature, tokens, n_given,
+                                            n_best, logprob, entropy, lse, top_ids, top_logprob, sm_count(), device_status,
+                                            static_cast<cudaStream_t>(cuda_stream));
+  g_launches.fetch_add(1);
+  if (e != cudaSuccess) {
+    (void)cudaGetLastError();
+    return SPECEXT_ERR_CUDA;
+  }
+  return SPECEXT_OK;
 }
 
 int specext_draft_attn(const specext_attn_desc* desc, const void* Q, const void* K_cache,

@@ -58,6 +58,39 @@ const at::Tensor& bf16_3d(PyObject* o, const char* what) {
   if (t.scalar_type() != at::kBFloat16 || t.dim() != 3 || t.stride(2) != 1) fail(what);
   return t;
 }
+// A prefix cache: bf16, or the codes of one in 8 bits.
+const at::Tensor& prefix_3d(PyObject* o) {
+  const at::Tensor& t = tensor(o);
+  if ((t.scalar_type() != at::kBFloat16 && t.scalar_type() != at::kFloat8_e4m3fn) || t.dim() != 3 || t.stride(2) != 1)
+    fail("K_prefix must be a bf16 (or float8_e4m3fn) [.][heads][head_dim] tensor with contiguous head_dim");
+  return t;
+}
+const at::Tensor& codes_3d(PyObject* o) {
+  const at::Tensor& t = cuda_tensor(o);
+  if (t.scalar_type() != at::kFloat8_e4m3fn || t.dim() != 3 || t.stride(2) != 1)
+    fail("codes must be float8_e4m3fn [.][heads][head_dim] with contiguous head_dim");
+  return t;
+}
+const at::Tensor& scales_2d(PyObject* o) {
+  const at::Tensor& t = cuda_tensor(o);
+  if (t.scalar_type() != at::kFloat8_e8m0fnu || t.dim() != 2) fail("scales must be float8_e8m0fnu [blocks][heads]");
+  return t;
+}
+// The 8-bit side of a call: codes and scales of K and V that belong together and hold `tokens` tokens of `heads` heads.
+specext_q8_desc q8_desc(const at::Tensor& Kc, const at::Tensor& Vc, const at::Tensor& Ks, const at::Tensor& Vs, int32_t block,
+                        int64_t tokens, int64_t heads, int64_t dim) {
+  if (Kc.strides() != Vc.strides() || Kc.sizes() != Vc.sizes() || Ks.strides() != Vs.strides() || Ks.sizes() != Vs.sizes())
+    fail("K and V must share the shapes and strides of their codes and scales");
+  const int64_t blocks = block > 0 ? (tokens + block - 1) / block : 0;       // (a bad block is refused by the library)
+  if (Kc.size(0) < tokens || Kc.size(1) != heads || Kc.size(2) != dim || Ks.size(0) < blocks || Ks.size(1) != heads)
+    fail("the cache does not hold that many tokens, heads or values: codes [tokens][heads][head_dim], scales [blocks][heads]");
+  specext_q8_desc q = {};
+  q.block_tokens = block;
+  // (a dimension of one has any stride)
+  q.scale_stride_b = Ks.size(0) > 1 ? Ks.stride(0) : heads;
+  q.scale_stride_h = heads > 1 ? Ks.stride(1) : 1;
+  return q;
+}
 const at::Tensor& draft_kv(PyObject* o) {
   const at::Tensor& t = cuda_tensor(o);
   if (t.scalar_type() != at::kBFloat16 || t.dim() != 4 || t.stride(3) != 1)
@@ -147,7 +180,7 @@ constexpr const char* kAttnTypes = "parent/device_status must be int32 and lse f
 PyObject* fill_desc(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 9, [&]() -> PyObject* {
     const at::Tensor& Q = bf16_3d(a[1], "Q must be a bf16 [.][heads][head_dim] tensor with contiguous head_dim");
-    const at::Tensor& K = bf16_3d(a[2], "K_prefix must be a bf16 [.][heads][head_dim] tensor with contiguous head_dim");
+    const at::Tensor& K = prefix_3d(a[2]);
     const at::Tensor& Kt = bf16_3d(a[3], "K_tree must be a bf16 [.][heads][head_dim] tensor with contiguous head_dim");
     const at::Tensor& O = bf16_3d(a[4], "O must be a bf16 [.][heads][head_dim] tensor with contiguous head_dim");
     Desc d(a[0], true);
@@ -210,6 +243,118 @@ PyObject* draft_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void *Q = ptr(a[2]), *K = ptr(a[3]), *V = ptr(a[4]), *Kt = ptr(a[6]), *Vt = ptr(a[7]), *O = ptr(a[9]);
     void* st = stream();
     return released([&] { return fn(d.get(), Q, K, V, n_tokens, Kt, Vt, parent, O, lse, ws, ws_bytes, status, st); });
+  });
+}
+
+// (entry, desc, Q, K_codes, V_codes, K_scale, V_scale, block_tokens, K_tree, V_tree, parent, O, lse, chunk_score, workspace,
+//  device_status)
+PyObject* verify_attn_q8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 16, [&]() -> PyObject* {
+    same_strides(a[9], a[8], kStrides);
+    const Desc d(a[1]);
+    const at::Tensor &Kc = codes_3d(a[3]), &Vc = codes_3d(a[4]), &Ks = scales_2d(a[5]), &Vs = scales_2d(a[6]);
+    const specext_q8_desc q = q8_desc(Kc, Vc, Ks, Vs, int32(a[7]), d.get()->prefix_len, d.get()->n_kv_heads, d.get()->head_dim);
+    if (d.get()->kv_stride_l != Kc.stride(0) || d.get()->kv_stride_h != Kc.stride(1)) fail("desc was made for another cache");
+    const int32_t* parent = i32(a[10], kAttnTypes);
+    float* lse = f32(a[12], kAttnTypes);
+    float* score = a[13] == Py_None ? nullptr : f32(a[13], "chunk_score must be fp32");
+    int32_t* status = i32(a[15], kAttnTypes);
+    void* ws = ptr(a[14]);
+    const size_t ws_bytes = tensor(a[14]).nbytes();
+    const auto fn = entry<decltype(&specext_verify_attn_q8)>(a[0]);
+    void *Q = ptr(a[2]), *Kt = ptr(a[8]), *Vt = ptr(a[9]), *O = ptr(a[11]);
+    void *kc = Kc.data_ptr(), *vc = Vc.data_ptr(), *ks = Ks.data_ptr(), *vs = Vs.data_ptr();
+    void* st = stream();
+    return released([&] {
+      return fn(d.get(), &q, Q, kc, vc, ks, vs, Kt, Vt, parent, O, lse, score, ws, ws_bytes, status, st);
+    });
+  });
+}
+
+// (entry, K, V, start, K_codes, V_codes, K_scale, V_scale, block_tokens, device_status, rows)
+PyObject* quantize_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 11, [&]() -> PyObject* {
+    const at::Tensor& K = bf16_3d(a[1], "K must be a bf16 [.][heads][head_dim] tensor with contiguous head_dim");
+    const at::Tensor& V = bf16_3d(a[2], "V must be a bf16 [.][heads][head_dim] tensor with contiguous head_dim");
+    if (K.strides() != V.strides() || K.sizes() != V.sizes()) fail("K and V must share shape and strides");
+    const int32_t start = int32(a[3]);
+    const at::Tensor &Kc = codes_3d(a[4]), &Vc = codes_3d(a[5]), &Ks = scales_2d(a[6]), &Vs = scales_2d(a[7]);
+    int64_t n_tokens = K.size(0);
+    const int32_t* rows = nullptr;
+    if (a[10] != Py_None) {
+      rows = i32(a[10], "rows must be a contiguous int32 vector");
+      if (tensor(a[10]).dim() != 1 || !tensor(a[10]).is_contiguous()) fail("rows must be a contiguous int32 vector");
+      n_tokens = tensor(a[10]).size(0);
+    }
+    if (start < 0 || K.size(0) > INT32_MAX || n_tokens > INT32_MAX) fail("start or the number of tokens is out of range");
+    const specext_q8_desc q = q8_desc(Kc, Vc, Ks, Vs, int32(a[8]), start + n_tokens, K.size(1), K.size(2));
+    int32_t* status = i32(a[9], "device_status must be int32");
+    const auto fn = entry<decltype(&specext_quantize_kv)>(a[0]);
+    void *k = ptr(a[1]), *v = ptr(a[2]), *kc = Kc.data_ptr(), *vc = Vc.data_ptr(), *ks = Ks.data_ptr(), *vs = Vs.data_ptr();
+    const int32_t n_src = (int32_t)K.size(0), heads = (int32_t)K.size(1), dim = (int32_t)K.size(2);
+    // (a dimension of one has any stride)
+    const int64_t s_l = n_src > 1 ? K.stride(0) : (int64_t)heads * dim, s_h = heads > 1 ? K.stride(1) : dim;
+    const int64_t c_l = Kc.size(0) > 1 ? Kc.stride(0) : (int64_t)heads * dim, c_h = heads > 1 ? Kc.stride(1) : dim;
+    void* st = stream();
+    return released([&] {
+      return fn(k, v, n_src, heads, dim, s_l, s_h, rows, (int32_t)n_tokens, start, kc, vc, c_l, c_h, ks, vs, &q, status, st);
+    });
+  });
+}
+
+// (entry, logits, tokens, logprob, entropy, lse, top_ids, top_logprob, device_status, temperature); tokens and logprob, and top_ids
+// and top_logprob, may be None
+PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 10, [&]() -> PyObject* {
+    const at::Tensor& x = cuda_tensor(a[1]);
+    const bool fp32 = x.scalar_type() == at::kFloat;
+    if ((!fp32 && x.scalar_type() != at::kBFloat16) || x.dim() != 2 || (x.size(1) > 1 && x.stride(1) != 1))
+      fail("logits must be bf16 or fp32 [rows][vocab] with contiguous words");
+    const int64_t rows = x.size(0), vocab = x.size(1);
+    if (rows > INT32_MAX || vocab > INT32_MAX) fail("logits have more rows or words than an int32 counts");
+    auto table = [&](PyObject* o, int64_t columns, const char* what) {     // contiguous [rows][columns]
+      const at::Tensor& t = tensor(o);
+      if (t.dim() != 2 || t.size(0) != rows || t.size(1) != columns || !t.is_contiguous()) fail(what);
+    };
+    if ((a[2] == Py_None) != (a[3] == Py_None) || (a[6] == Py_None) != (a[7] == Py_None))
+      fail("tokens and logprob, top_ids and top_logprob go together");
+    constexpr const char* given_text = "tokens must be contiguous int32 [rows][given] and logprob fp32 of the same shape";
+    constexpr const char* best_text = "top_ids must be contiguous int32 [rows][best] and top_logprob fp32 of the same shape";
+    const int32_t* tokens = nullptr;
+    float *logprob = nullptr, *top_logprob = nullptr;
+    int32_t* top_ids = nullptr;
+    int64_t given = 0, best = 0;
+    if (a[2] != Py_None) {
+      tokens = i32(a[2], given_text);
+      logprob = f32(a[3], given_text);
+      if (tensor(a[2]).dim() != 2) fail(given_text);
+      given = tensor(a[2]).size(1);
+      table(a[2], given, given_text);
+      table(a[3], given, given_text);
+    }
+    if (a[6] != Py_None) {
+      top_ids = i32(a[6], best_text);
+      top_logprob = f32(a[7], best_text);
+      if (tensor(a[6]).dim() != 2) fail(best_text);
+      best = tensor(a[6]).size(1);
+      table(a[6], best, best_text);
+      table(a[7], best, best_text);
+    }
+    if (given > INT32_MAX || best > INT32_MAX) fail(given_text);
+    constexpr const char* stat_text = "entropy and lse must be contiguous fp32 vectors with a value for each row";
+    float *entropy = f32(a[4], stat_text), *lse = f32(a[5], stat_text);
+    for (int i = 4; i < 6; ++i)
+      if (tensor(a[i]).numel() < rows || !tensor(a[i]).is_contiguous()) fail(stat_text);
+    int32_t* status = i32(a[8], "device_status must be int32");
+    const float temperature = real(a[9]);
+    const auto fn = entry<decltype(&specext_token_logprobs)>(a[0]);
+    const void* logits = x.data_ptr();
+    const int64_t stride = rows > 1 ? x.stride(0) : vocab;
+    void* st = stream();
+    return released([&] {
+      return fn(logits, fp32, (int32_t)rows, (int32_t)vocab, stride, temperature, tokens, (int32_t)given, (int32_t)best, logprob,
+                entropy, lse, top_ids, top_logprob, status, st);
+    });
   });
 }
 
@@ -292,6 +437,9 @@ PyMethodDef kMethods[] = {
     {"verify_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(verify_attn)), METH_FASTCALL, nullptr},
     {"draft_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(draft_attn)), METH_FASTCALL, nullptr},
     {"prefill_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(prefill_attn)), METH_FASTCALL, nullptr},
+    {"verify_attn_q8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(verify_attn_q8)), METH_FASTCALL, nullptr},
+    {"quantize_kv", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(quantize_kv)), METH_FASTCALL, nullptr},
+    {"token_logprobs", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(token_logprobs)), METH_FASTCALL, nullptr},
     {"select_gather", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(select_gather)), METH_FASTCALL, nullptr},
     {"current_stream", current_stream, METH_NOARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};

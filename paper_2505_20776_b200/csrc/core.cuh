@@ -135,15 +135,16 @@ __device__ __forceinline__ void tma_load_hint(uint32_t dst, const CUtensorMap* m
 // ---- set-up and end of a CTA ---------------------------------------------------------------------------
 // Barriers by the producer warp, tensor memory by the MMA warp, and the cluster barrier (block barrier) that publishes
 // them.  None of it touches global memory: it runs ahead of the dependency wait, under the kernel before.
-// HANDOVER: segments end with segment_handover (else segment_end).
-template <int PAIR, bool HANDOVER = false>
+// HANDOVER: segments end with segment_handover (else segment_end).  FILLERS: arrivals of each CTA that fill a stage of K or V, or
+// Q (one TMA producer, or the warps that convert what it brought).
+template <int PAIR, bool HANDOVER = false, int FILLERS = 1>
 __device__ __forceinline__ void setup(Ctrl* ctl, int warp, int lane) {
   constexpr int kEnd = HANDOVER ? 4 : 4 * kWG;    // warps of a CTA that take part in the end of a segment
   if (warp == kProducerWarp) {
     if (lane < kMaxStages) {
-      mbar_init(&ctl->k_full[lane], PAIR);
+      mbar_init(&ctl->k_full[lane], FILLERS * PAIR);
       mbar_init(&ctl->k_empty[lane], 1);
-      mbar_init(&ctl->v_full[lane], PAIR);
+      mbar_init(&ctl->v_full[lane], FILLERS * PAIR);
       mbar_init(&ctl->v_empty[lane], 1);
     } else if (lane < kMaxStages + kWG) {
       const int i = lane - kMaxStages;
@@ -153,7 +154,7 @@ __device__ __forceinline__ void setup(Ctrl* ctl, int warp, int lane) {
       mbar_init(&ctl->pv_done[i], 1);
       mbar_init(&ctl->m_pub[i], 4);
     } else if (lane == kMaxStages + kWG) {
-      mbar_init(&ctl->q_full, PAIR);
+      mbar_init(&ctl->q_full, FILLERS * PAIR);
       mbar_init(&ctl->q_empty, 1);
       mbar_init(&ctl->o_done, 1);
       mbar_init(&ctl->o_free, kEnd * PAIR);
@@ -204,13 +205,11 @@ __device__ __forceinline__ void finish(Ctrl* ctl, int warp) {
 // Two threads of the leader CTA issue the S and the PV MMAs.  (A thread that issues an MMA is held until the tensor pipe
 // takes it, and its waits, commits and bookkeeping cost it another ~0.5 K cycles a tile: one thread for both kinds left
 // the pipe idle that long, 2.1 K cycles a tile against 1.0 K of MMAs.)  `Work` enumerates the segments (`next()`, `n`
-// tiles in the current one).
-template <int PAIR, int D, class Work>
-__device__ __forceinline__ bool issue_s(Ctrl* ctl, unsigned char* base, const Geo<PAIR, D>& geo, Work work,
-                                        volatile int* abort_flag) {
-  using G = Geo<PAIR, D>;
+// tiles in the current one).  F16: the operands are f16 instead of bf16.
+template <int PAIR, int D, bool F16 = false, class G, class Work>
+__device__ __forceinline__ bool issue_s(Ctrl* ctl, unsigned char* base, const G& geo, Work work, volatile int* abort_flag) {
   const uint32_t tmem = ctl->tmem_base;
-  const uint32_t idesc = idesc_bf16_f32(128 * PAIR, SPX_TILE_KEYS, false, false);
+  const uint32_t idesc = idesc_f32<F16>(128 * PAIR, SPX_TILE_KEYS, false, false);
   constexpr uint32_t hi = desc_hi(1024);
   const uint32_t q_lo = desc_lo(smem_u32(base), 16), q_blk = geo.q_blk >> 4;
   const uint32_t k_lo = desc_lo(smem_u32(base + geo.k_off), 16);
@@ -250,12 +249,10 @@ __device__ __forceinline__ bool issue_s(Ctrl* ctl, unsigned char* base, const Ge
   commit<PAIR>(&ctl->drain);
   return ok;
 }
-template <int PAIR, int D, class Work>
-__device__ __forceinline__ bool issue_pv(Ctrl* ctl, unsigned char* base, const Geo<PAIR, D>& geo, Work work,
-                                         volatile int* abort_flag) {
-  using G = Geo<PAIR, D>;
+template <int PAIR, int D, bool F16 = false, class G, class Work>
+__device__ __forceinline__ bool issue_pv(Ctrl* ctl, unsigned char* base, const G& geo, Work work, volatile int* abort_flag) {
   const uint32_t tmem = ctl->tmem_base, d = tmem + kColO;
-  const uint32_t idesc = idesc_bf16_f32(128 * PAIR, D, false, true);
+  const uint32_t idesc = idesc_f32<F16>(128 * PAIR, D, false, true);
   constexpr uint32_t hi = desc_hi(1024);
   const uint32_t v_lo = desc_lo(smem_u32(base + geo.v_off), PAIR == 2 ? 16 : G::kVBlk);
   int vst = 0, w = 0;

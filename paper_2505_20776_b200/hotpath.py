@@ -7,11 +7,12 @@ scores), then SelectChunks for the accepted node's row, then UpdateDraftCache.
 """
 from __future__ import annotations
 
-from typing import Dict, Optional
+from typing import Dict, Optional, Tuple
 
 import torch
 
 from . import api
+from .cache8 import KvCache8
 
 
 class HotPath:
@@ -70,6 +71,31 @@ class HotPath:
         cs = self._score_flat if want_score else None
         api.specext_verify_attn(d, t["Q"], t["K_prefix"], t["V_prefix"], t["K_tree"], t["V_tree"], parent,
                                 self.O, self.lse, cs, self._ws, self.status)
+
+    def verify_attn_q8(self, t: Dict[str, torch.Tensor], cache: KvCache8, parent: torch.Tensor, want_score: bool) -> None:
+        """verify_attn with the prefix (all tokens of `cache`) in 8 bits; t needs Q, K_tree and V_tree only."""
+        if cache.length > self.max_prefix:
+            raise ValueError("prefix_len exceeds max_prefix")
+        d = api.make_attn_desc(t["Q"], cache.K, t["K_tree"], self.O, cache.length, self.C, self.scale, want_score)
+        need = api.specext_verify_attn_q8_workspace(d, cache.block_tokens)
+        if need == 0:
+            raise api.SpecextError(2, "specext_verify_attn_q8_workspace")
+        if self._ws.numel() < need:
+            self._ws = self._alloc((need,), torch.uint8)
+        api.specext_verify_attn_q8(d, t["Q"], cache.K, cache.V, cache.K_scale, cache.V_scale, cache.block_tokens, t["K_tree"],
+                                   t["V_tree"], parent, self.O, self.lse, self._score_flat if want_score else None, self._ws,
+                                   self.status)
+
+    def token_logprobs(self, logits: torch.Tensor, tokens: Optional[torch.Tensor], n_best: int, temperature: float = 1.0
+                       ) -> Tuple[Optional[torch.Tensor], torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
+        """(logprob like tokens or None, entropy [rows], lse [rows], top_ids [rows][n_best], top_logprob) of rows of logits:
+        what the target's logits say of the tree's tokens, and the draft's of how to expand it."""
+        rows = logits.shape[0]
+        lp = None if tokens is None else self._alloc(tuple(tokens.shape), torch.float32)
+        entropy, lse = self._alloc((rows,), torch.float32), self._alloc((rows,), torch.float32)
+        ids, best = self._alloc((rows, n_best), torch.int32), self._alloc((rows, n_best), torch.float32)
+        api.specext_token_logprobs(logits, tokens, lp, entropy, lse, ids, best, self.status, temperature)
+        return lp, entropy, lse, ids, best
 
     def select_chunks(self, row: int, prefix_len: int, n_sink_chunks: int = 0, n_recent_chunks: int = 0) -> None:
         api.specext_select_chunks(self.chunk_score(prefix_len), row, prefix_len, self.C, self.k, self.idx,
