@@ -17,8 +17,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libspecext.so")
 BINDING_PATH = os.path.join(HERE, "_binding.so")
 TESTING_LIB_PATH = os.path.join(HERE, "libspecext_testing.so")
-SOURCES = ["api.cu", "attn_tc2.cu", "verify.cu", "prefill.cu", "merge.cu", "retrieval.cu", "verify_q8.cu", "quantize.cu",
-           "logprob.cu"]
+SOURCES = ["api.cu", "attn_tc2.cu", "verify.cu", "prefill.cu", "merge.cu", "retrieval.cu", "verify_q8.cu", "rows_q8.cu",
+           "quantize.cu", "logprob.cu"]
 TESTING_SOURCES = SOURCES + ["attn_simt.cu", "testing.cu"]
 
 

@@ -287,6 +287,53 @@ int build_plan(const specext_attn_desc* d, AttnPlan* out, bool dev_len = false) 
 bool q8_strides(long long a, long long b, int head_dim) { return a >= head_dim && b >= head_dim && ((a | b) & 15) == 0; }
 int block_log2(int block_tokens) { return block_tokens == 32 ? 5 : block_tokens == 64 ? 6 : block_tokens == 128 ? 7 : 0; }
 
+// Workers and workspace of the plan: p.cpp workers a problem, or clusters of `cluster` that merge among themselves.
+void lay_out_rows_workspace(AttnPlan* plan, int cluster) {
+  AttnPlan& p = *plan;
+  p.cluster = cluster;
+  if (cluster > 0) p.cpp = cluster;
+  p.n_cta = p.NP * p.cpp;
+  p.q = p.UPP / p.cpp;
+  p.rem = p.UPP % p.cpp;
+  p.max_segs = p.cpp;
+  lay_out_workspace(plan);
+}
+
+// Few rows (rows_q8.cu): units are groups of 16 keys, prefix and tree alike.
+int lay_out_rows_q8(AttnPlan* plan) {
+  AttnPlan& p = *plan;
+  p.kernel = 5;
+  p.RB = p.q_rows = kSpxRowsQ8;
+  p.n_rblk = 1;
+  p.NP = p.Hkv;
+  p.TPH = (p.L + 15) / 16;
+  p.UPP = p.TPH + (p.T + 15) / 16;
+  if ((long long)p.NP * p.UPP > (1ll << 30)) return SPECEXT_ERR_UNSUPPORTED;
+  p.U = p.NP * p.UPP;
+  p.cpp = sm_count() / p.NP;
+  if (p.cpp > (p.UPP + 7) / 8) p.cpp = (p.UPP + 7) / 8;
+  if (p.cpp < 1) p.cpp = 1;
+  int dev = -1, size = 0;
+  if (cudaGetDevice(&dev) == cudaSuccess) {
+    for (int s = 16; s >= 1 && size == 0; --s)
+      if (s <= p.cpp && p.NP <= spx_rows_q8_max_clusters(dev, s)) size = s;
+  } else {
+    (void)cudaGetLastError();
+  }
+  lay_out_rows_workspace(&p, 0);
+  const long long split_floats = p.total_floats;           // (the workspace does not depend on what clusters the device holds)
+  // The clusters merge among themselves, which saves 1.5 to 3 us with the second launch, but they leave SMs idle (eight of ten CTAs
+  // are all that fit at once), so that a warp takes more steps of 16 keys.  us per call, replayed, split / cluster (steps): 32
+  // query / 8 KV heads, one node: 1K 6.9 / 5.1, 16K 12.9 / 12.1 (8 / 13), 128K 48.4 / 48.4 (57 / 103: HBM either way); 16 / 2 heads:
+  // 4K 9.2 / 5.7, 32K 14.5 / 12.8 (4 / 17), 128K 21.9 / 37.9 (14 / 65); 12 x 64 heads: 16K 11.3 / 10.8 (11 / 15), 64K 27.7 / 30.9
+  // (43 / 57).  More than 8 rows make a step longer: 16 rows at 8K 11.8 / 10.9 (4 / 7), 16K 15.0 / 15.2 (8 / 13); 32 rows at
+  // 8K 20.5 / 18.7, 16K 27.0 / 29.1.
+  const int split_steps = (p.UPP + 8 * p.cpp - 1) / (8 * p.cpp), steps = size > 0 ? (p.UPP + 8 * size - 1) / (8 * size) : 0;
+  if (size > 0 && steps - split_steps <= (p.rows <= 8 ? 13 : 4)) lay_out_rows_workspace(&p, size);
+  if (p.total_floats < split_floats) p.total_floats = split_floats;
+  return SPECEXT_OK;
+}
+
 // The plan of an attention call on the 8-bit cache: every problem has the same whole number of workers.
 int build_plan_q8(const specext_attn_desc* d, const specext_q8_desc* q, AttnPlan* out) {
   AttnPlan p;
@@ -295,6 +342,10 @@ int build_plan_q8(const specext_attn_desc* d, const specext_q8_desc* q, AttnPlan
   if (!q || block_log2(q->block_tokens) == 0) return q ? SPECEXT_ERR_UNSUPPORTED : SPECEXT_ERR_INVALID_ARG;
   if (!q8_strides(d->kv_stride_l, d->kv_stride_h, d->head_dim) || q->scale_stride_b < 1 || q->scale_stride_h < 1)
     return SPECEXT_ERR_INVALID_ARG;
+  if (p.rows <= kSpxRowsQ8 && !p.want_score) {
+    *out = p;
+    return lay_out_rows_q8(out);
+  }
   p.kernel = 4;
   p.RB = p.q_rows = 128;
   p.n_rblk = (p.rows + p.RB - 1) / p.RB;
@@ -455,7 +506,7 @@ int specext_verify_attn_q8(const specext_attn_desc* desc, const specext_q8_desc*
   q.log_block = block_log2(q8->block_tokens);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   int n = 0;
-  cudaError_t e = spx_launch_verify_q8(q, st, &n);
+  cudaError_t e = p.kernel == 5 ? spx_launch_rows_q8(q, st, &n) : spx_launch_verify_q8(q, st, &n);
   if (e == cudaSuccess) e = spx_launch_merge(a, st, &n);
   g_launches.fetch_add(n);
   if (e != cudaSuccess) {

@@ -7,6 +7,7 @@
 #define SPECEXT_Q8_CUH_
 
 #include "common.cuh"
+#include "sm100.cuh"
 
 struct Q8Args {
   AttnArgs a;                                   // (Kp, Vp unused)
@@ -21,7 +22,8 @@ __device__ __forceinline__ float e8m0_value(uint32_t code) {
   return __uint_as_float(code == 255u ? 0x7fc00000u : code << 23);
 }
 __device__ __forceinline__ float e8m0_log2(uint32_t code) {
-  return code == 255u ? __uint_as_float(0x7fc00000u) : (float)((int)code - 127);
+  // (2^23 + code, less 2^23 + 127: an integer conversion takes longer)
+  return code == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(0x4b000000u | code) - 8388735.0f;
 }
 
 // Two e4m3 codes as two f16 values: every e4m3 value is one.
@@ -31,6 +33,31 @@ __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t codes) {
   return r;
 }
 
-cudaError_t spx_launch_verify_q8(const Q8Args& q, cudaStream_t st, int* n_launches);
+// bf16 values go to f16 with a power of two 2^-e: the e for which the largest finite magnitude `amax` (bits of a non-negative
+// float) comes to lie in [2^14, 2^15); 0 for zeros.
+__device__ __forceinline__ int f16_exponent(uint32_t amax) {
+  const int e = (int)(amax >> 23) - 127 - 14;
+  return amax == 0u ? 0 : max(e, -126);
+}
+__device__ __forceinline__ float exp2_int(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }    // -126 <= e <= 127
+
+// Magnitude bits of the two bf16 of a word as floats, non-finite ones as zero; the larger of both and `m`.
+__device__ __forceinline__ uint32_t amax_bf16x2(uint32_t m, uint32_t w) {
+  uint32_t lo = (w << 16) & 0x7fffffffu, hi = w & 0x7fff0000u;
+  if (lo >= 0x7f800000u) lo = 0u;
+  if (hi >= 0x7f800000u) hi = 0u;
+  return max(m, max(lo, hi));
+}
+__device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t w, float f) {
+  return sm100::pack_f16x2(__uint_as_float(w << 16) * f, __uint_as_float(w & 0xffff0000u) * f);
+}
+__device__ __forceinline__ uint4 bf16x8_to_f16x8(uint4 x, float f) {
+  return make_uint4(bf16x2_to_f16x2(x.x, f), bf16x2_to_f16x2(x.y, f), bf16x2_to_f16x2(x.z, f), bf16x2_to_f16x2(x.w, f));
+}
+
+cudaError_t spx_launch_verify_q8(const Q8Args& q, cudaStream_t st, int* n_launches);      // any rows, chunk sums
+cudaError_t spx_launch_rows_q8(const Q8Args& q, cudaStream_t st, int* n_launches);        // up to kSpxRowsQ8 rows, no chunk sums
+constexpr int kSpxRowsQ8 = 32;
+int spx_rows_q8_max_clusters(int dev, int size);
 
 #endif  // SPECEXT_Q8_CUH_

@@ -84,28 +84,6 @@ struct OneRun {
   }
 };
 
-// 2^-e of the largest finite magnitude `amax` of some values (bits of a non-negative float), such that amax 2^-e lies in
-// [2^14, 2^15); 1 for zeros.
-__device__ __forceinline__ int f16_exponent(uint32_t amax) {
-  const int e = (int)(amax >> 23) - 127 - 14;
-  return amax == 0u ? 0 : max(e, -126);
-}
-__device__ __forceinline__ float exp2_int(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }    // -126 <= e <= 127
-
-// Magnitude bits of the two bf16 of a word as floats, non-finite ones as zero; the larger of both and `m`.
-__device__ __forceinline__ uint32_t amax_bf16x2(uint32_t m, uint32_t w) {
-  uint32_t lo = (w << 16) & 0x7fffffffu, hi = w & 0x7fff0000u;
-  if (lo >= 0x7f800000u) lo = 0u;
-  if (hi >= 0x7f800000u) hi = 0u;
-  return max(m, max(lo, hi));
-}
-__device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t w, float f) {
-  return pack_f16x2(__uint_as_float(w << 16) * f, __uint_as_float(w & 0xffff0000u) * f);
-}
-__device__ __forceinline__ uint4 bf16x8_to_f16x8(uint4 x, float f) {
-  return make_uint4(bf16x2_to_f16x2(x.x, f), bf16x2_to_f16x2(x.y, f), bf16x2_to_f16x2(x.z, f), bf16x2_to_f16x2(x.w, f));
-}
-
 // Place of 16-byte column `col` (of D * 2 / 16) of row `row` in a K or V stage, or in Q: blocks of 64 elements, 128-byte swizzle.
 __device__ __forceinline__ int f16_place(int row, int col) { return (col >> 3) * (128 * 128) + row * 128 + (((col ^ row) & 7) << 4); }
 
