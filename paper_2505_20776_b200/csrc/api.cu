@@ -346,14 +346,17 @@ int build_plan_q8(const specext_attn_desc* d, const specext_q8_desc* q, AttnPlan
     *out = p;
     return lay_out_rows_q8(out);
   }
+  // one CTA on 128-row blocks, or pairs of CTAs on 256-row blocks for head_dim 128 and more than 128 rows
+  const bool pair = p.D == 128 && p.rows > 128;
   p.kernel = 4;
-  p.RB = p.q_rows = 128;
+  p.RB = pair ? 256 : 128;
+  p.q_rows = 128;
   p.n_rblk = (p.rows + p.RB - 1) / p.RB;
   const long long np = (long long)p.Hkv * p.n_rblk;
   if (np * p.UPP > (1ll << 30)) return SPECEXT_ERR_UNSUPPORTED;
   p.NP = (int)np;
   p.U = p.NP * p.UPP;
-  p.cpp = sm_count() / p.NP;
+  p.cpp = (pair ? sm_count() / 2 : sm_count()) / p.NP;
   if (p.cpp > p.UPP) p.cpp = p.UPP;
   if (p.cpp < 1) p.cpp = 1;
   p.n_cta = p.NP * p.cpp;

@@ -6,6 +6,8 @@
 #ifndef SPECEXT_Q8_CUH_
 #define SPECEXT_Q8_CUH_
 
+#include <cuda_fp16.h>
+
 #include "common.cuh"
 #include "sm100.cuh"
 
@@ -54,6 +56,14 @@ __device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t w, float f) {
 __device__ __forceinline__ uint4 bf16x8_to_f16x8(uint4 x, float f) {
   return make_uint4(bf16x2_to_f16x2(x.x, f), bf16x2_to_f16x2(x.y, f), bf16x2_to_f16x2(x.z, f), bf16x2_to_f16x2(x.w, f));
 }
+
+// Two floats as e4m3, rounded to nearest even; |x| <= 448.
+__device__ __forceinline__ uint32_t f32x2_to_e4m3x2(float lo, float hi) {
+  unsigned short r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float2 f16x2_to_f32x2(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
 
 cudaError_t spx_launch_verify_q8(const Q8Args& q, cudaStream_t st, int* n_launches);      // any rows, chunk sums
 cudaError_t spx_launch_rows_q8(const Q8Args& q, cudaStream_t st, int* n_launches);        // up to kSpxRowsQ8 rows, no chunk sums

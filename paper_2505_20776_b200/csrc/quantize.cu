@@ -31,19 +31,13 @@ __device__ __forceinline__ uint32_t scale_code(uint32_t amax_bits) {
   return e < kScaleFloor + 8 ? kScaleFloor : e - 8;
 }
 
-__device__ __forceinline__ uint32_t f32x2_to_e4m3x2(float lo, float hi) {
-  unsigned short r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-  return r;
-}
 __device__ __forceinline__ uint32_t bf16x4_to_e4m3x4(uint32_t a, uint32_t b, float f) {
   return f32x2_to_e4m3x2(__uint_as_float(a << 16) * f, __uint_as_float(a & 0xffff0000u) * f) |
          (f32x2_to_e4m3x2(__uint_as_float(b << 16) * f, __uint_as_float(b & 0xffff0000u) * f) << 16);
 }
 // Four codes times f.
 __device__ __forceinline__ uint32_t scaled_e4m3x4(uint32_t codes, float f) {
-  const uint32_t lo = e4m3x2_to_f16x2(codes), hi = e4m3x2_to_f16x2(codes >> 16);
-  const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&lo)), y = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+  const float2 x = f16x2_to_f32x2(e4m3x2_to_f16x2(codes)), y = f16x2_to_f32x2(e4m3x2_to_f16x2(codes >> 16));
   return f32x2_to_e4m3x2(x.x * f, x.y * f) | (f32x2_to_e4m3x2(y.x * f, y.y * f) << 16);
 }
 

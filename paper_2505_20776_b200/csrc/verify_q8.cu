@@ -1,22 +1,23 @@
-// Hybrid Tree Attention over a prefix cache in 8 bits (codes e4m3, scales e8m0, see q8.cuh), on the pipeline of core.cuh with one
-// CTA per worker: partial attention of 128 stacked (query head x tree node) rows of one KV head against a run of 128-key tiles.
+// Hybrid Tree Attention over a prefix cache in 8 bits (codes e4m3, scales e8m0, see q8.cuh), on the pipeline of core.cuh: partial
+// attention of 128 stacked (query head x tree node) rows of one KV head by a CTA, or of 256 by a pair of CTAs (tcgen05
+// cta_group::2, each staging half of every key tile), against a run of 128-key tiles.
 //
-// The tensor cores multiply f16.  e4m3 values are f16 values, so a tile is expanded by one conversion per two codes and no
-// rounding; bf16 would take four integer instructions and a multiplication (a conversion and an integer instruction cost the
-// same two cycles a warp, and the expansion is what this kernel does more of than the one for bf16).  The scales stay outside:
-//   S = (q 2^-e) . k_code                          e: the row's own power of two, so that bf16 queries are exact in f16
-//   z = S * (scale log2(e) 2^e k_scale) + log2(v_scale)
+// S = Q K^T is a product of e4m3 by e4m3, twice: a bf16 value has 8 significant bits and is the sum of two e4m3 values of 4, so
+// with the query row taken to [2^7, 2^8) by a power of two its high and low parts, multiplied with the codes as they lie in
+// memory, give S as exactly as bf16 products would (elements 2^-10 of the row's largest and less are kept to 2^-18 of it), in the
+// time of the bf16 products and without touching K.  The tree's bf16 keys are two such tiles, high parts and low parts.
+// For O += P V the codes of V become f16 (every e4m3 value is one: one conversion per two codes) by four warps, and P is f16.
+// The scales stay outside the products:
+//   z = S * (scale log2(e) 2^e k_scale) + log2(v_scale)          e: the query row's own power of two
 //   P = 2^(z - M) rounded to f16,  O += P v_code,  l += 2^(z - M) / v_scale
 // with M the reference maximum of z: the V scale rides on the exponent, at no cost per element, and P stays in f16's range
 // whatever the scales are.  M is 2^6 below the maximum it was taken from and may fall 2^8 more behind, so P is at most 2^14;
 // f16 keeps 11 bits down to 2^-20 of the row's largest weight and reaches 2^-30.
-// The tree's bf16 keys and values become f16 with a power of two for each group of 32 (finite values decide it).
+// (First both K and V were expanded to f16, by the same four warps: 2.7 us a tile of 128 keys against 0.75 for its bytes.)
 //
 // Warps: 0-7 softmax, 8 TMA producer of the codes, 9 issuer of the S MMAs, 10 of the PV MMAs, 11 ancestor masks and TMA
-// producer of Q, 12-15 expansion (a thread has a key: codes from the staging ring, f16 into the K or V stage; Q, a thread has a
-// row, in place).  Every wait is bounded; all threads reach the final barrier before tensor memory is freed.
-#include <cstddef>
-
+// producer of Q, 12-15 expansion (Q: a thread has a row; V: a thread has a key; the tree's keys and values).  Every wait is
+// bounded; all threads reach the final barrier before tensor memory is freed.
 #include "core.cuh"
 #include "q8.cuh"
 #include "tmap.h"
@@ -31,46 +32,46 @@ constexpr int kRegsLaunchQ8 = 128, kRegsOtherQ8 = 48, kRegsSoftmaxQ8 = 208;
 static_assert(256 * (kRegsLaunchQ8 - kRegsOtherQ8) >= 256 * (kRegsSoftmaxQ8 - kRegsLaunchQ8),
               "setmaxnreg.inc would wait for registers that are never released");
 constexpr float kHeadroom = 6.0f;              // log2: how far the reference lies below the maximum it was taken from
-constexpr int kMaxUnits = 8, kScaleSlots = 8;
+constexpr int kMaxUnits = 8;
 
 struct Q8Maps {
   CUtensorMap q, k, v;
 };
 
-// Shared memory: Q | K stages | V stages (f16) | staging ring of code tiles | control.
-template <int D>
+// Shared memory: Q (high parts, low parts) | V stages (f16) | ring of K codes | ring of V codes | control.  A unit of K is what
+// this CTA has of a tile's keys, whole; one of V its columns of all 128 keys.
+template <int PAIR, int D>
 struct GeoQ8 {
   static constexpr int kBlocks = D / 64;
-  static constexpr int kKBlk = SPX_TILE_KEYS * 128, kVBlk = kKBlk;
-  static constexpr int kKStage = kKBlk * kBlocks, kVStage = kKStage;
-  static constexpr int q_blk = 128 * 128;
-  static constexpr int nk = D == 128 ? 2 : 3, nv = nk;
-  static constexpr uint32_t k_off = q_blk * kBlocks, v_off = k_off + nk * kKStage;
-  static constexpr uint32_t st_off = v_off + nv * kVStage;
-  static constexpr int kUnit = SPX_TILE_KEYS * D, kUnits = D == 128 ? 3 : 8;
-  static constexpr int kCtrl = st_off + kUnits * kUnit;
+  static constexpr int kQ = 128 * D;                                   // one part
+  static constexpr int kVRow = PAIR == 2 ? 64 : D;                     // bytes of a key in a unit of V
+  static constexpr int kVBlk = SPX_TILE_KEYS * 128, kVStage = kVBlk * (kVRow / 64);
+  static constexpr int kKUnit = SPX_TILE_KEYS / PAIR * D, kVUnit = SPX_TILE_KEYS * kVRow;
+  static constexpr int nv = kVStage == 32768 ? 2 : 3;
+  static constexpr int kKUnits = kKUnit == 16384 ? 4 : 6, kVUnits = kVUnit == 16384 ? 3 : 6;
+  static constexpr uint32_t v_off = 2 * kQ, k8_off = v_off + nv * kVStage, v8_off = k8_off + kKUnits * kKUnit;
+  static constexpr int kCtrl = v8_off + kVUnits * kVUnit;
+  static_assert(nv * kVStage >= 2 * kQ, "the V stages hold the bf16 queries in the beginning");
 };
 
 // Scales of a tile, per group of 32 keys.
-struct alignas(16) Q8Scales {
+struct Q8Scales {
   float k[4], v_log2[4], v_inv[4];
 };
 struct CtrlQ8 {
-  Ctrl c;
-  uint64_t st_full[kMaxUnits], st_empty[kMaxUnits];
-  uint64_t q_land;
-  // by tile, modulo kScaleSlots: tile t + 8 is expanded only after the S MMA of tile t + 6, hence after the warpgroup of tile t
-  // has taken the scores of tile t + 4
-  Q8Scales sc[kScaleSlots];
+  Ctrl c;                                      // (its K ring is not used; v_full, v_empty: the f16 stages)
+  uint64_t k_full[kMaxUnits];                  // leader: one arrival per CTA (the producer's with its bytes, or the tree's)
+  uint64_t k_empty[kMaxUnits];                 // each CTA: MMA completion
+  uint64_t vc_full[kMaxUnits], vc_empty[kMaxUnits];      // this CTA: codes of V, between the producer and the expansion
+  uint64_t q_land;                             // this CTA: the bf16 queries have landed
+  int tree_k[4], tree_v[4];                    // exponents of the tree's groups
   float q_scale[128];
 };
 constexpr int kCtrlBytesQ8 = 8192;
 static_assert(sizeof(CtrlQ8) <= kCtrlBytesQ8, "control block too large");
-static_assert(sizeof(Q8Scales) == 48 && offsetof(CtrlQ8, sc) % 16 == 0, "scales are read as float4");
-static_assert(GeoQ8<64>::kCtrl % 1024 == 0 && GeoQ8<128>::kCtrl % 1024 == 0, "stages begin on 1024 bytes");
-template <int D>
+template <int PAIR, int D>
 constexpr int smem_q8() {
-  return GeoQ8<D>::kCtrl + kCtrlBytesQ8 + 1024;
+  return GeoQ8<PAIR, D>::kCtrl + kCtrlBytesQ8 + 1024;
 }
 
 // A worker has one run of tiles of one problem.
@@ -84,47 +85,146 @@ struct OneRun {
   }
 };
 
-// Place of 16-byte column `col` (of D * 2 / 16) of row `row` in a K or V stage, or in Q: blocks of 64 elements, 128-byte swizzle.
-__device__ __forceinline__ int f16_place(int row, int col) { return (col >> 3) * (128 * 128) + row * 128 + (((col ^ row) & 7) << 4); }
-
-// One key's codes from a staged tile (rows of D bytes, swizzled as TMA left them) as f16 into a stage.
-template <int D>
-__device__ __forceinline__ void expand_key(const unsigned char* unit, unsigned char* stage, int key) {
-#pragma unroll 4
-  for (int c = 0; c < D / 16; ++c) {
-    const int at = D == 128 ? c ^ (key & 7) : c ^ ((key >> 1) & 3);
-    const uint4 x = *reinterpret_cast<const uint4*>(unit + key * D + (at << 4));
-    *reinterpret_cast<uint4*>(stage + f16_place(key, 2 * c)) =
-        make_uint4(e4m3x2_to_f16x2(x.x), e4m3x2_to_f16x2(x.x >> 16), e4m3x2_to_f16x2(x.y), e4m3x2_to_f16x2(x.y >> 16));
-    *reinterpret_cast<uint4*>(stage + f16_place(key, 2 * c + 1)) =
-        make_uint4(e4m3x2_to_f16x2(x.z), e4m3x2_to_f16x2(x.z >> 16), e4m3x2_to_f16x2(x.w), e4m3x2_to_f16x2(x.w >> 16));
+// ---- forms of the instructions for e4m3 and for a pair -----------------------------------------------------
+template <int PAIR>
+__device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
+  if constexpr (PAIR == 2)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+        "mov.b64 da, {%1, %3};\n\t"
+        "mov.b64 db, {%2, %3};\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], da, db, %4, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+        "mov.b64 da, {%1, %3};\n\t"
+        "mov.b64 db, {%2, %3};\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %4, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// A warp's arrival on a barrier of the leader, behind its plain stores to shared memory that the pair's MMAs read.
+template <int PAIR>
+__device__ __forceinline__ void publish(uint64_t* bar, int lane) {
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncwarp();
+  if (lane == 0) {
+    if constexpr (PAIR == 2) arrive_release_cluster(map_to_cta(smem_u32(bar), 0));
+    else mbar_arrive(bar);
   }
 }
 
-// The power of two that takes the bf16 keys or values of a warp's 32 tree nodes to f16 (a lane has one; its row of D).
+// Place of 16-byte column `col` of row `row` in a block of f16 (or bf16): blocks of 64 elements, 128-byte swizzle.
+__device__ __forceinline__ int f16_place(int row, int col) { return (col >> 3) * (128 * 128) + row * 128 + (((col ^ row) & 7) << 4); }
+// Place of 16-byte piece `c` of row `row` in a tile of codes, rows of W bytes, swizzled as TMA leaves them.
+template <int W>
+__device__ __forceinline__ int code_place(int row, int c) {
+  return row * W + ((W == 128 ? c ^ (row & 7) : c ^ ((row >> 1) & 3)) << 4);
+}
+
+// One key's codes (W of them) as f16 into a stage.
+template <int W>
+__device__ __forceinline__ void expand_key(const unsigned char* unit, unsigned char* stage, int key) {
+#pragma unroll
+  for (int c = 0; c < W / 16; c += 2) {
+    uint4 x[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) x[i] = *reinterpret_cast<const uint4*>(unit + code_place<W>(key, c + i));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      *reinterpret_cast<uint4*>(stage + f16_place(key, 2 * (c + i))) = make_uint4(
+          e4m3x2_to_f16x2(x[i].x), e4m3x2_to_f16x2(x[i].x >> 16), e4m3x2_to_f16x2(x[i].y), e4m3x2_to_f16x2(x[i].y >> 16));
+      *reinterpret_cast<uint4*>(stage + f16_place(key, 2 * (c + i) + 1)) = make_uint4(
+          e4m3x2_to_f16x2(x[i].z), e4m3x2_to_f16x2(x[i].z >> 16), e4m3x2_to_f16x2(x[i].w), e4m3x2_to_f16x2(x[i].w >> 16));
+    }
+  }
+}
+
+// bf16 values to e4m3: the power of two 2^-e that takes the largest finite magnitude to [2^7, 2^8).
+__device__ __forceinline__ int e4m3_exponent(uint32_t amax) {
+  const int e = (int)(amax >> 23) - 127 - 7;
+  return amax == 0u ? 0 : max(e, -126);
+}
+__device__ __forceinline__ uint32_t amax_bf16x8(uint32_t m, uint4 x) {
+  return amax_bf16x2(amax_bf16x2(amax_bf16x2(amax_bf16x2(m, x.x), x.y), x.z), x.w);
+}
+// High and low parts of four bf16 values times f.
+__device__ __forceinline__ void split4(uint32_t a, uint32_t b, float f, uint32_t& hi, uint32_t& lo) {
+  const float x0 = __uint_as_float(a << 16) * f, x1 = __uint_as_float(a & 0xffff0000u) * f;
+  const float x2 = __uint_as_float(b << 16) * f, x3 = __uint_as_float(b & 0xffff0000u) * f;
+  const uint32_t h0 = f32x2_to_e4m3x2(x0, x1), h1 = f32x2_to_e4m3x2(x2, x3);
+  const uint32_t w0 = e4m3x2_to_f16x2(h0), w1 = e4m3x2_to_f16x2(h1);
+  const float2 y0 = f16x2_to_f32x2(w0), y1 = f16x2_to_f32x2(w1);
+  hi = h0 | (h1 << 16);
+  lo = f32x2_to_e4m3x2(x0 - y0.x, x1 - y0.y) | (f32x2_to_e4m3x2(x2 - y1.x, x3 - y1.y) << 16);
+}
+// 16 bf16 values (two 16-byte pieces) as a piece of high parts and one of low parts.
+__device__ __forceinline__ void split16(uint4 x, uint4 y, float f, unsigned char* hi, unsigned char* lo) {
+  uint4 h, l;
+  split4(x.x, x.y, f, h.x, l.x);
+  split4(x.z, x.w, f, h.y, l.y);
+  split4(y.x, y.y, f, h.z, l.z);
+  split4(y.z, y.w, f, h.w, l.w);
+  *reinterpret_cast<uint4*>(hi) = h;
+  *reinterpret_cast<uint4*>(lo) = l;
+}
+
+// The largest finite magnitude in the rows of a warp's 32 tree nodes (a lane has one).
 template <int D>
-__device__ __forceinline__ int tree_exponent(const __nv_bfloat16* src, bool valid) {
+__device__ __forceinline__ uint32_t tree_amax(const __nv_bfloat16* src, bool valid) {
   uint32_t m = 0u;
   const uint4* row = reinterpret_cast<const uint4*>(src);
 #pragma unroll 4
-  for (int c = 0; c < D / 8; ++c) {
-    const uint4 x = valid ? row[c] : make_uint4(0u, 0u, 0u, 0u);
-    m = amax_bf16x2(amax_bf16x2(amax_bf16x2(amax_bf16x2(m, x.x), x.y), x.z), x.w);
-  }
-  return f16_exponent(__reduce_max_sync(0xffffffffu, m));
+  for (int c = 0; c < D / 8; ++c) m = amax_bf16x8(m, valid ? row[c] : make_uint4(0u, 0u, 0u, 0u));
+  return __reduce_max_sync(0xffffffffu, m);
 }
-// One tree node's key or value as f16 into a stage.
-template <int D>
-__device__ __forceinline__ void expand_node(const __nv_bfloat16* src, bool valid, unsigned char* stage, int key, float f) {
-  const uint4* row = reinterpret_cast<const uint4*>(src);
-#pragma unroll 4
-  for (int c = 0; c < D / 8; ++c)
-    *reinterpret_cast<uint4*>(stage + f16_place(key, c)) = bf16x8_to_f16x8(valid ? row[c] : make_uint4(0u, 0u, 0u, 0u), f);
+
+// Issuer of the S MMAs.  has_tree: the last tile of the run is the tree's, two units of K.
+template <int PAIR, int D>
+__device__ __forceinline__ bool issue_s_q8(CtrlQ8* ctl8, unsigned char* base, int n_tiles, bool has_tree, volatile int* abort_flag) {
+  using G = GeoQ8<PAIR, D>;
+  Ctrl* ctl = &ctl8->c;
+  constexpr uint32_t idesc = idesc_f32<true>(128 * PAIR, SPX_TILE_KEYS, false, false);     // (e4m3: type fields 0 as for f16)
+  // rows of D bytes, 8-row groups of 8 D; 128-byte swizzle, or 64-byte (mode 4) for D = 64
+  constexpr uint32_t hi = D == 128 ? desc_hi(1024) : ((512u >> 4) | (1u << 14) | (4u << 29));
+  const uint32_t q_lo = desc_lo(smem_u32(base), 16), k_lo = desc_lo(smem_u32(base + G::k8_off), 16);
+  int st = 0;
+  uint32_t ph = 0;
+  bool ok = wait_c(&ctl->q_full, 0, abort_flag);
+  for (int j = 0; j < n_tiles && ok; ++j) {
+    const int w = j & 1, units = has_tree && j == n_tiles - 1 ? 2 : 1;
+    // the rows of the tile before last are in registers: its S buffer is free
+    if (j >= kWG) ok = wait_c(&ctl->s_free[w], (j / kWG - 1) & 1, abort_flag);
+    const uint32_t d = ctl->tmem_base + kColS + w * 128;
+    for (int u = 0; u < units && ok; ++u) {
+      ok = wait_c(&ctl8->k_full[st], ph, abort_flag);
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t kb = k_lo + st * (G::kKUnit >> 4);
+#pragma unroll
+      for (int part = 0; part < 2; ++part)
+#pragma unroll
+        for (int kk = 0; kk < D / 32; ++kk)
+          mma_f8<PAIR>(d, q_lo + part * (G::kQ >> 4) + kk * 2, kb + kk * 2, hi, idesc, part + kk > 0 || u > 0 ? 1u : 0u);
+      commit<PAIR>(&ctl8->k_empty[st]);
+      if (++st == G::kKUnits) {
+        st = 0;
+        ph ^= 1;
+      }
+    }
+    if (ok) commit<PAIR>(&ctl->s_full[w]);
+  }
+  commit<PAIR>(&ctl->drain);
+  return ok;
 }
 
 // softmax_tile of core.cuh with scales: `mult` is the row's factor (softmax scale, log2 e, the power of two of the query row).
 template <int D, class MaskFn, class SumFn>
-__device__ __forceinline__ bool softmax_tile_q8(const RowCtx& rc, const Q8Scales* sc, float mult, uint32_t t, bool need_mask,
+__device__ __forceinline__ bool softmax_tile_q8(const RowCtx& rc, const Q8Scales& sc, float mult, uint32_t t, bool need_mask,
                                                 MaskFn&& mask, SumFn&& sums, float& m_loc, float& l) {
   Ctrl* ctl = rc.ctl;
   const int w = rc.w, wp = w ^ 1;
@@ -137,7 +237,6 @@ __device__ __forceinline__ bool softmax_tile_q8(const RowCtx& rc, const Q8Scales
   tmem_ld32(s_addr + 32, s1);
   tmem_ld32(s_addr + 64, s2);
   tmem_ld32(s_addr + 96, s3);
-  const float4 ks = *reinterpret_cast<const float4*>(sc->k), ev = *reinterpret_cast<const float4*>(sc->v_log2);
   float m_cur = -INFINITY;
   if (!first) {
     if (!mbar_wait(&ctl->m_pub[wp], ((t - 1) / kWG) & 1, rc.abort_flag)) return false;
@@ -163,9 +262,9 @@ __device__ __forceinline__ bool softmax_tile_q8(const RowCtx& rc, const Q8Scales
     }
     return fmaxf(a, b);
   };
-  const float f0 = mult * ks.x, f1 = mult * ks.y, f2 = mult * ks.z, f3 = mult * ks.w;
-  const float m_tile = fmaxf(fmaxf(fmaf(max_group(s0), f0, ev.x), fmaf(max_group(s1), f1, ev.y)),
-                             fmaxf(fmaf(max_group(s2), f2, ev.z), fmaf(max_group(s3), f3, ev.w))) - kHeadroom;
+  const float f0 = mult * sc.k[0], f1 = mult * sc.k[1], f2 = mult * sc.k[2], f3 = mult * sc.k[3];
+  const float m_tile = fmaxf(fmaxf(fmaf(max_group(s0), f0, sc.v_log2[0]), fmaf(max_group(s1), f1, sc.v_log2[1])),
+                             fmaxf(fmaf(max_group(s2), f2, sc.v_log2[2]), fmaf(max_group(s3), f3, sc.v_log2[3]))) - kHeadroom;
 
   float m_new = m_cur;
   bool rescale = false;
@@ -220,7 +319,7 @@ __device__ __forceinline__ bool softmax_tile_q8(const RowCtx& rc, const Q8Scales
     float gs0, gs1, gs2, gs3;
     unpack_f32x2(acc01, gs0, gs1);
     unpack_f32x2(acc23, gs2, gs3);
-    const float inv = sc->v_inv[c], gs = ((gs0 + gs1) + (gs2 + gs3)) * inv;
+    const float inv = sc.v_inv[c], gs = ((gs0 + gs1) + (gs2 + gs3)) * inv;
     l += gs;
     sums(c, v, gs, inv);
     uint32_t pk[16];
@@ -228,10 +327,10 @@ __device__ __forceinline__ bool softmax_tile_q8(const RowCtx& rc, const Q8Scales
     for (int k = 0; k < 16; ++k) pk[k] = pack_f16x2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1]));
     tmem_st16(p_addr + c * 16, pk);
   };
-  exp_chunk(s0, 0, f0, ev.x - m_new);
-  exp_chunk(s1, 1, f1, ev.y - m_new);
-  exp_chunk(s2, 2, f2, ev.z - m_new);
-  exp_chunk(s3, 3, f3, ev.w - m_new);
+  exp_chunk(s0, 0, f0, sc.v_log2[0] - m_new);
+  exp_chunk(s1, 1, f1, sc.v_log2[1] - m_new);
+  exp_chunk(s2, 2, f2, sc.v_log2[2] - m_new);
+  exp_chunk(s3, 3, f3, sc.v_log2[3] - m_new);
   tmem_wait_st();
   tc_fence_before();
   warp_arrive_cluster(rc.p_full, rc.lane);
@@ -239,10 +338,10 @@ __device__ __forceinline__ bool softmax_tile_q8(const RowCtx& rc, const Q8Scales
 }
 
 // SCORE: as in verify.cu: 0 no chunk sums, 1 chunks of 32 keys, 2 of 64 or 128, 3 of fewer than 32.
-template <int D, int SCORE>
+template <int PAIR, int D, int SCORE>
 __global__ void __launch_bounds__(kThreadsQ8, 1)
 verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8Maps maps) {
-  using G = GeoQ8<D>;
+  using G = GeoQ8<PAIR, D>;
   const AttnArgs& a = args.a;
   const AttnPlan& p = a.plan;
   extern __shared__ unsigned char smem_raw[];
@@ -254,101 +353,117 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const G geo;
 
-  const int worker = blockIdx.x, prob = worker / p.cpp;
+  const int rank = PAIR == 2 ? (int)cluster_rank() : 0;
+  const int worker = blockIdx.x / PAIR, prob = worker / p.cpp;
   const int unit_lo = spx_unit_start(p, worker), n_tiles = spx_unit_start(p, worker + 1) - unit_lo;
   const int tile_lo = unit_lo - prob * p.UPP, g = prob / p.n_rblk, rblk = prob - g * p.n_rblk;
+  const bool has_tree = tile_lo + n_tiles == p.UPP;
+  const int n_pref = n_tiles - (has_tree ? 1 : 0);
   if (warp == kTreeWarp) {
     if (lane < kMaxUnits) {
-      mbar_init(&ctl8->st_full[lane], 1);
-      mbar_init(&ctl8->st_empty[lane], 4);
+      mbar_init(&ctl8->k_full[lane], PAIR);
+      mbar_init(&ctl8->k_empty[lane], 1);
+      mbar_init(&ctl8->vc_full[lane], 1);
+      mbar_init(&ctl8->vc_empty[lane], 4);
     } else if (lane == kMaxUnits) {
       mbar_init(&ctl8->q_land, 1);
     }
     fence_mbar_init();
   }
-  setup<1, false, 4>(ctl, warp, lane);
+  setup<PAIR, false, 4>(ctl, warp, lane);
   pdl_launch_dependents();
   bool ok = true;
   OneRun work{n_tiles, false};
 
   if (warp >= kExpandWarp) {
-    // ================================ expansion to f16 ========================================
+    // ================================ queries, V and the tree in the tensor cores' types ======
     setmaxnreg_dec<kRegsOtherQ8>();
     const int group = warp - kExpandWarp, key = group * 32 + lane;
-    auto scale_of = [&](const uint8_t* s, int tile) -> uint32_t {
-      const int token = tile * SPX_TILE_KEYS + group * 32;
-      return tile < p.TPH && token < p.L ? s[(long long)(token >> args.log_block) * args.s_sb + (long long)g * args.s_sh] : 127u;
-    };
     pdl_wait();
-    uint32_t ks = scale_of(args.Ks, tile_lo), vs = scale_of(args.Vs, tile_lo);
     ok = mbar_wait(&ctl8->q_land, 0, abort_flag);
     if (ok) {
+      const unsigned char* q = base + G::v_off;          // (bf16, where V's stages will be)
       uint32_t m = 0u;
 #pragma unroll 4
-      for (int c = 0; c < D / 8; ++c) {
-        const uint4 x = *reinterpret_cast<const uint4*>(base + f16_place(key, c));
-        m = amax_bf16x2(amax_bf16x2(amax_bf16x2(amax_bf16x2(m, x.x), x.y), x.z), x.w);
-      }
-      const int e = f16_exponent(m);
+      for (int c = 0; c < D / 8; ++c) m = amax_bf16x8(m, *reinterpret_cast<const uint4*>(q + f16_place(key, c)));
+      const int e = e4m3_exponent(m);
       const float f = exp2_int(-e);
-#pragma unroll 4
-      for (int c = 0; c < D / 8; ++c) {
-        uint4* x = reinterpret_cast<uint4*>(base + f16_place(key, c));
-        *x = bf16x8_to_f16x8(*x, f);
-      }
+#pragma unroll 2
+      for (int c = 0; c < D / 16; ++c)
+        split16(*reinterpret_cast<const uint4*>(q + f16_place(key, 2 * c)), *reinterpret_cast<const uint4*>(q + f16_place(key, 2 * c + 1)),
+                f, base + code_place<D>(key, c), base + G::kQ + code_place<D>(key, c));
       ctl8->q_scale[key] = exp2_int(e);
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      warp_arrive(&ctl->q_full, lane);
+      publish<PAIR>(&ctl->q_full, lane);
     }
-    int st = 0, kst = 0, vst = 0;
-    uint32_t stph = 0, kph = 1, vph = 1;
-    for (int j = 0; j < n_tiles && ok; ++j) {
-      const int tile = tile_lo + j;
-      const bool is_tree = tile == p.TPH, node = key < p.T;
-      Q8Scales* sc = &ctl8->sc[j & (kScaleSlots - 1)];
-      const uint32_t ks_next = scale_of(args.Ks, tile + 1), vs_next = scale_of(args.Vs, tile + 1);
-      const long long node_at = (long long)key * a.tkv_st + (long long)g * a.tkv_sh;
-      int ke = 0, ve = 0;
-      if (is_tree) {
-        ke = tree_exponent<D>(a.Kt + node_at, node);
-        ve = tree_exponent<D>(a.Vt + node_at, node);
-      }
-#pragma unroll 1
-      for (int half = 0; half < 2 && ok; ++half) {
-        // K, then V
-        uint64_t* full = half ? &ctl->v_full[vst] : &ctl->k_full[kst];
-        unsigned char* stage = base + (half ? G::v_off + vst * G::kVStage : G::k_off + kst * G::kKStage);
-        if (!is_tree) ok = mbar_wait(&ctl8->st_full[st], stph, abort_flag);
-        if (ok) ok = half ? wait_c(&ctl->v_empty[vst], vph, abort_flag) : wait_c(&ctl->k_empty[kst], kph, abort_flag);
-        if (!ok) break;
-        // (the scales of K and of V: both are read as soon as the tile's scores are there)
-        if (lane == 0 && half == 0) {
-          sc->k[group] = is_tree ? exp2_int(ke) : e8m0_value(ks);
-          sc->v_log2[group] = is_tree ? (float)ve : e8m0_log2(vs);
-          sc->v_inv[group] = is_tree ? exp2_int(-ve) : e8m0_value(vs == 255u ? 255u : 254u - vs);
-        }
-        if (is_tree) expand_node<D>((half ? a.Vt : a.Kt) + node_at, node, stage, key, exp2_int(half ? -ve : -ke));
-        else expand_key<D>(base + G::st_off + st * G::kUnit, stage, key);
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        warp_arrive(full, lane);
-        if (!is_tree) {
-          if (lane == 0) mbar_arrive(&ctl8->st_empty[st]);
-          if (++st == G::kUnits) {
-            st = 0;
-            stph ^= 1;
-          }
-        }
-      }
-      if (++kst == G::nk) {
-        kst = 0;
-        kph ^= 1;
+    named_bar_sync(1, 128);                              // everybody has read the bf16 queries
+    int vc = 0, vst = 0;
+    uint32_t vcph = 0, vph = 1;
+    for (int j = 0; j < n_pref && ok; ++j) {
+      ok = mbar_wait(&ctl8->vc_full[vc], vcph, abort_flag) && wait_c(&ctl->v_empty[vst], vph, abort_flag);
+      if (!ok) break;
+      expand_key<G::kVRow>(base + G::v8_off + vc * G::kVUnit, base + G::v_off + vst * G::kVStage, key);
+      publish<PAIR>(&ctl->v_full[vst], lane);
+      if (lane == 0) mbar_arrive(&ctl8->vc_empty[vc]);
+      if (++vc == G::kVUnits) {
+        vc = 0;
+        vcph ^= 1;
       }
       if (++vst == G::nv) {
         vst = 0;
         vph ^= 1;
       }
-      ks = ks_next;
-      vs = vs_next;
+    }
+    if (has_tree) {
+      // (no early way out: the meetings below are everybody's)
+      const __nv_bfloat16* kt = a.Kt + (long long)g * a.tkv_sh;
+      const __nv_bfloat16* vt = a.Vt + (long long)g * a.tkv_sh;
+      const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+      {
+        const bool node = key < p.T;
+        const uint32_t km = tree_amax<D>(kt + (long long)key * a.tkv_st, node), vm = tree_amax<D>(vt + (long long)key * a.tkv_st, node);
+        if (lane == 0) {
+          ctl8->tree_k[group] = e4m3_exponent(km);
+          ctl8->tree_v[group] = f16_exponent(vm);
+        }
+      }
+      named_bar_sync(1, 128);
+      // K: high and low parts, two units of the ring behind those of the prefix
+      int u[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int pos = n_pref + i;
+        u[i] = pos % G::kKUnits;
+        if (ok) ok = wait_c(&ctl8->k_empty[u[i]], ((pos / G::kKUnits) & 1) ^ 1, abort_flag);
+      }
+      if (ok) {
+        // PAIR: this CTA's 64 keys, half of the columns a thread
+        const int row = PAIR == 2 ? key & 63 : key, at = PAIR == 2 ? rank * 64 + row : key;
+        const int c0 = PAIR == 2 ? (key >> 6) * (D / 32) : 0;
+        const uint4* src = reinterpret_cast<const uint4*>(kt + (long long)at * a.tkv_st);
+        const float f = exp2_int(-ctl8->tree_k[at >> 5]);
+#pragma unroll 2
+        for (int c = c0; c < c0 + D / 16 / PAIR; ++c)
+          split16(at < p.T ? src[2 * c] : none, at < p.T ? src[2 * c + 1] : none, f,
+                  base + G::k8_off + u[0] * G::kKUnit + code_place<D>(row, c), base + G::k8_off + u[1] * G::kKUnit + code_place<D>(row, c));
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      named_bar_sync(1, 128);
+      if (ok && key == 0) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if constexpr (PAIR == 2) arrive_release_cluster(map_to_cta(smem_u32(&ctl8->k_full[u[i]]), 0));
+          else mbar_arrive(&ctl8->k_full[u[i]]);
+        }
+      }
+      if (ok) ok = wait_c(&ctl->v_empty[vst], vph, abort_flag);
+      if (ok) {
+        const uint4* src = reinterpret_cast<const uint4*>(vt + (long long)key * a.tkv_st) + rank * 8;
+        const float f = exp2_int(-ctl8->tree_v[group]);
+#pragma unroll 4
+        for (int c = 0; c < G::kVRow / 8; ++c)
+          *reinterpret_cast<uint4*>(base + G::v_off + vst * G::kVStage + f16_place(key, c)) = bf16x8_to_f16x8(key < p.T ? src[c] : none, f);
+        publish<PAIR>(&ctl->v_full[vst], lane);
+      }
     }
     if (*abort_flag) ok = false;
   } else if (warp == kProducerWarp) {
@@ -357,41 +472,56 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
     pdl_wait();
     if (lane == 0) {
       const uint64_t stream_once = policy_evict_first();
-      const uint32_t full0 = smem_u32(&ctl8->st_full[0]), ring = smem_u32(base + G::st_off);
-      int st = 0;
-      uint32_t ph = 1;
-      for (int u = 0; u < 2 * n_tiles && ok; ++u) {
-        const int tile = tile_lo + (u >> 1);
-        if (tile == p.TPH) break;                        // the tree's keys and values are not staged
-        ok = wait_c(&ctl8->st_empty[st], ph, abort_flag);
+      const uint32_t kbar = leader_addr<PAIR>(&ctl8->k_full[0]), vbar = smem_u32(&ctl8->vc_full[0]);
+      const uint32_t kring = smem_u32(base + G::k8_off), vring = smem_u32(base + G::v8_off);
+      int ks = 0, vs = 0;
+      uint32_t kph = 1, vph = 1;
+      for (int j = 0; j < n_pref && ok; ++j) {
+        const int key0 = (tile_lo + j) * SPX_TILE_KEYS;
+        ok = wait_c(&ctl8->k_empty[ks], kph, abort_flag);
         if (!ok) break;
-        arrive_expect_tx_cluster(full0 + st * 8, G::kUnit);
-        tma_load_hint<1>(ring + st * G::kUnit, u & 1 ? &maps.v : &maps.k, full0 + st * 8, 0, g, tile * SPX_TILE_KEYS, stream_once);
-        if (++st == G::kUnits) {
-          st = 0;
-          ph ^= 1;
+        arrive_expect_tx_cluster(kbar + ks * 8, G::kKUnit);
+        tma_load_hint<PAIR>(kring + ks * G::kKUnit, &maps.k, kbar + ks * 8, 0, g, key0 + rank * (SPX_TILE_KEYS / PAIR), stream_once);
+        if (++ks == G::kKUnits) {
+          ks = 0;
+          kph ^= 1;
+        }
+        ok = wait_c(&ctl8->vc_empty[vs], vph, abort_flag);
+        if (!ok) break;
+        arrive_expect_tx_cluster(vbar + vs * 8, G::kVUnit);
+        tma_load_hint<1>(vring + vs * G::kVUnit, &maps.v, vbar + vs * 8, rank * 64, g, key0, stream_once);
+        if (++vs == G::kVUnits) {
+          vs = 0;
+          vph ^= 1;
         }
       }
       if (*abort_flag) ok = false;
     }
   } else if (warp == kMmaWarp) {
     setmaxnreg_dec<kRegsOtherQ8>();
-    pdl_wait();
-    if (lane == 0) ok = issue_s<1, D, true>(ctl, base, geo, work, abort_flag);
+    pdl_wait();                                          // (a bounded wait must not count the time of the kernel before)
+    if (lane == 0 && rank == 0) ok = issue_s_q8<PAIR, D>(ctl8, base, n_tiles, has_tree, abort_flag);
   } else if (warp == kPvWarp) {
     setmaxnreg_dec<kRegsOtherQ8>();
+    if (lane == 0) {
+      // the first tiles are asked for in L2 ahead of the dependency wait, by a thread that has nothing else to do yet
+      for (int j = 0; j < min(n_pref, 2); ++j) {
+        tma_prefetch_3d(&maps.k, 0, g, (tile_lo + j) * SPX_TILE_KEYS + rank * (SPX_TILE_KEYS / PAIR));
+        tma_prefetch_3d(&maps.v, rank * 64, g, (tile_lo + j) * SPX_TILE_KEYS);
+      }
+    }
     pdl_wait();
-    if (lane == 0) ok = issue_pv<1, D, true>(ctl, base, geo, work, abort_flag);
+    if (lane == 0 && rank == 0) ok = issue_pv<PAIR, D, true>(ctl, base, geo, work, abort_flag);
   } else if (warp == kTreeWarp) {
     // ================================ ancestor masks, TMA producer of Q =======================
     setmaxnreg_dec<kRegsOtherQ8>();
     pdl_wait();
     if (lane == 0) {
       const uint32_t bar = smem_u32(&ctl8->q_land);
-      arrive_expect_tx_cluster(bar, G::q_blk * G::kBlocks);
+      arrive_expect_tx_cluster(bar, 128 * 128 * G::kBlocks);
 #pragma unroll
       for (int ds = 0; ds < G::kBlocks; ++ds)
-        tma_load<1>(smem_u32(base + ds * G::q_blk), &maps.q, bar, 64 * ds, g * p.G, rblk * p.RB / p.G);
+        tma_load<1>(smem_u32(base + G::v_off + ds * 128 * 128), &maps.q, bar, 64 * ds, g * p.G, (rblk * p.RB + rank * 128) / p.G);
     }
     __syncwarp();
 #pragma unroll
@@ -418,11 +548,11 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
     rc.lane = lane;
     rc.row_t = quarter * 32 + lane;
     rc.lane_tmem = ctl->tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
-    rc.s_free = smem_u32(&ctl->s_free[rc.w]);
-    rc.p_full = smem_u32(&ctl->p_full[rc.w]);
+    rc.s_free = leader_addr<PAIR>(&ctl->s_free[rc.w]);
+    rc.p_full = leader_addr<PAIR>(&ctl->p_full[rc.w]);
     rc.scale2 = p.scale2;
     rc.abort_flag = abort_flag;
-    const int rr = rc.row_t, r = rblk * p.RB + rr;
+    const int rr = rank * 128 + rc.row_t, r = rblk * p.RB + rr;
     const bool valid = r < p.rows, warp_valid = r - lane < p.rows;
     rc.pad = !valid;
     if (!warp_valid) {
@@ -435,7 +565,14 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
       tmem_wait_st();
       tc_fence_before();
     }
+    // Scales of a tile: lane c has that of K's group c, lane 4 + c of V's, fetched two tiles ahead.
+    const uint8_t* s_src = (lane & 4 ? args.Vs : args.Ks) + (long long)g * args.s_sh;
+    auto scale_of = [&](int j) -> uint32_t {
+      const int token = (tile_lo + j) * SPX_TILE_KEYS + (lane & 3) * 32;
+      return lane < 8 && j < n_pref && token < p.L ? s_src[(long long)(token >> args.log_block) * args.s_sb] : 127u;
+    };
     pdl_wait();
+    uint32_t codes = scale_of(rc.w);
     const int t_node = valid ? r / p.G : 0;
     float m_loc = -INFINITY, l = 0.f, mult = 0.f;
     bool known = false;                                  // mult is the row's
@@ -447,16 +584,24 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
       const int tile = tile_lo + j;
       const bool is_tree = tile == p.TPH;
       const int nkeys = is_tree ? p.T : min(SPX_TILE_KEYS, p.L - tile * SPX_TILE_KEYS);
-      if (is_tree) {
-        ok = mbar_wait(&ctl->anc_ready, 0, abort_flag);
+      const uint32_t codes_next = scale_of(j + kWG);
+      if (!known || is_tree) {
+        // (the scores are there, so the query rows and the tree's scales are)
+        ok = mbar_wait(&ctl->s_full[rc.w], (j / kWG) & 1, abort_flag);
+        if (ok && is_tree) ok = mbar_wait(&ctl->anc_ready, 0, abort_flag);
         if (!ok) break;
-      }
-      if (!known) {
-        ok = mbar_wait(&ctl->q_full, 0, abort_flag);
-        if (!ok) break;
-        mult = p.scale2 * ctl8->q_scale[rr];
+        mult = p.scale2 * ctl8->q_scale[rc.row_t];
         known = true;
       }
+      Q8Scales sc;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const uint32_t kc = __shfl_sync(0xffffffffu, codes, c), vcode = __shfl_sync(0xffffffffu, codes, 4 + c);
+        sc.k[c] = is_tree ? exp2_int(ctl8->tree_k[c]) : e8m0_value(kc);
+        sc.v_log2[c] = is_tree ? (float)ctl8->tree_v[c] : e8m0_log2(vcode);
+        sc.v_inv[c] = is_tree ? exp2_int(-ctl8->tree_v[c]) : e8m0_value(vcode == 255u ? 255u : 254u - vcode);
+      }
+      codes = codes_next;
       float cg[4];                                       // sums of the tile's four groups of 32 keys
       float* mass = nullptr;
       long long rowbase = 0;
@@ -465,7 +610,7 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
         mass = a.ws + p.off_mass + rowbase * p.CPT;
       }
       ok = softmax_tile_q8<D>(
-          rc, &ctl8->sc[j & (kScaleSlots - 1)], mult, j, is_tree || nkeys < SPX_TILE_KEYS,
+          rc, sc, mult, j, is_tree || nkeys < SPX_TILE_KEYS,
           [&](unsigned long long& lo, unsigned long long& hi) {
             if (is_tree) {                 // this node and its ancestors (a padding row sees key 0)
               lo = valid ? ctl->anc[t_node][0] : 1ull;
@@ -535,50 +680,59 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
     if (lane == 0) spx_raise(a.status, SPECEXT_ERR_TIMEOUT);
     settle();
   }
-  finish<1>(ctl, warp);
+  finish<PAIR>(ctl, warp);
 }
 
-template <int D, int SCORE>
+template <int PAIR, int D, int SCORE>
 cudaError_t launch(const Q8Args& q, const Q8Maps& maps, cudaStream_t st) {
   static SpxOncePerDevice once;
-  constexpr int smem = smem_q8<D>();
+  constexpr int smem = smem_q8<PAIR, D>();
   static_assert(smem <= 232448, "more shared memory than a CTA can have");
-  const cudaError_t ec = spx_opt_in_smem(verify_q8_kernel<D, SCORE>, smem, &once);
+  const cudaError_t ec = spx_opt_in_smem(verify_q8_kernel<PAIR, D, SCORE>, smem, &once);
   if (ec != cudaSuccess) return ec;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(q.a.plan.n_cta);
+  cfg.gridDim = dim3(q.a.plan.n_cta * PAIR);
   cfg.blockDim = dim3(kThreadsQ8);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = PAIR;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, verify_q8_kernel<D, SCORE>, q, maps);
+  cfg.numAttrs = PAIR == 2 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, verify_q8_kernel<PAIR, D, SCORE>, q, maps);
 }
 
-template <int D>
+template <int PAIR, int D>
 cudaError_t launch_class(const Q8Args& q, const Q8Maps& maps, cudaStream_t st) {
   const AttnPlan& p = q.a.plan;
-  if (!p.want_score) return launch<D, 0>(q, maps, st);
-  return p.C == 32 ? launch<D, 1>(q, maps, st) : p.C > 32 ? launch<D, 2>(q, maps, st) : launch<D, 3>(q, maps, st);
+  if (!p.want_score) return launch<PAIR, D, 0>(q, maps, st);
+  return p.C == 32  ? launch<PAIR, D, 1>(q, maps, st)
+         : p.C > 32 ? launch<PAIR, D, 2>(q, maps, st)
+                    : launch<PAIR, D, 3>(q, maps, st);
 }
 
 }  // namespace
 
+// Row blocks of 128, or of 256 on pairs of CTAs (plan.RB); plan.n_cta counts CTAs, or pairs.
 cudaError_t spx_launch_verify_q8(const Q8Args& q, cudaStream_t st, int* n_launches) {
   const AttnArgs& a = q.a;
   const AttnPlan& p = a.plan;
+  const bool pair = p.RB == 256;
   Q8Maps maps;
   bool ok = spx_encode_map(&maps.q, a.Q, p.D, p.Hq, a.q_sh, p.T, a.q_st, p.G, 128 / p.G);
   if (p.L > 0) {
-    ok = ok && spx_encode_map8(&maps.k, q.Kc, p.D, p.Hkv, a.kv_sh, p.L, a.kv_sl, p.D, SPX_TILE_KEYS);
-    ok = ok && spx_encode_map8(&maps.v, q.Vc, p.D, p.Hkv, a.kv_sh, p.L, a.kv_sl, p.D, SPX_TILE_KEYS);
+    ok = ok && spx_encode_map8(&maps.k, q.Kc, p.D, p.Hkv, a.kv_sh, p.L, a.kv_sl, p.D, pair ? SPX_TILE_KEYS / 2 : SPX_TILE_KEYS);
+    ok = ok && spx_encode_map8(&maps.v, q.Vc, p.D, p.Hkv, a.kv_sh, p.L, a.kv_sl, pair ? 64 : p.D, SPX_TILE_KEYS);
   } else {
     maps.k = maps.v = maps.q;                            // never used
   }
   if (!ok) return cudaErrorInvalidValue;
   *n_launches += 1;
-  return p.D == 128 ? launch_class<128>(q, maps, st) : launch_class<64>(q, maps, st);
+  if (pair) return launch_class<2, 128>(q, maps, st);
+  return p.D == 128 ? launch_class<1, 128>(q, maps, st) : launch_class<1, 64>(q, maps, st);
 }
