@@ -357,8 +357,8 @@ int build_plan_q8(const specext_attn_desc* d, const specext_q8_desc* q, AttnPlan
   p.NP = (int)np;
   p.U = p.NP * p.UPP;
   p.cpp = (pair ? sm_count() / 2 : sm_count()) / p.NP;
+  if (p.cpp < (p.UPP + kSpxRunQ8 - 1) / kSpxRunQ8) p.cpp = (p.UPP + kSpxRunQ8 - 1) / kSpxRunQ8;
   if (p.cpp > p.UPP) p.cpp = p.UPP;
-  if (p.cpp < 1) p.cpp = 1;
   p.n_cta = p.NP * p.cpp;
   p.q = p.UPP / p.cpp;
   p.rem = p.UPP % p.cpp;

@@ -63,8 +63,19 @@ __device__ __forceinline__ uint32_t f32x2_to_e4m3x2(float lo, float hi) {
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
   return r;
 }
+__device__ __forceinline__ uint32_t f16x2_to_e4m3x2(uint32_t x) {
+  unsigned short r;
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(x));
+  return r;
+}
+__device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("sub.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
 __device__ __forceinline__ float2 f16x2_to_f32x2(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
 
+constexpr int kSpxRunQ8 = 144;                      // tiles of a worker's run (their scales are kept in shared memory)
 cudaError_t spx_launch_verify_q8(const Q8Args& q, cudaStream_t st, int* n_launches);      // any rows, chunk sums
 cudaError_t spx_launch_rows_q8(const Q8Args& q, cudaStream_t st, int* n_launches);        // up to kSpxRowsQ8 rows, no chunk sums
 constexpr int kSpxRowsQ8 = 32;

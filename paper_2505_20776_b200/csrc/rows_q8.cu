@@ -487,13 +487,11 @@ rows_q8_kernel(const __grid_constant__ Q8Args args) {
   int stage = 0;
 #pragma unroll 1
   for (int unit = first; unit < staged_end; unit += kWarps) {
-    uint32_t ks_next = 127u, vs_next = 127u;
-    ks_src += s_step;
-    vs_src += s_step;
     if (unit + kWarps < staged_end) {
-      ks_next = *ks_src;
-      vs_next = *vs_src;
+      ks_src += s_step;
+      vs_src += s_step;
     }
+    const uint32_t ks_next = *ks_src, vs_next = *vs_src;
     copies_wait<G::kStages - 2>();
     __syncwarp();
     staged_step<D, NR>(st, ring_ptr + stage * G::kStage, p.L - unit * kGroupKeys, e8m0_value(ks), e8m0_log2(vs),

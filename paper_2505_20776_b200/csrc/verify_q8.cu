@@ -15,9 +15,9 @@
 // f16 keeps 11 bits down to 2^-20 of the row's largest weight and reaches 2^-30.
 // (First both K and V were expanded to f16, by the same four warps: 2.7 us a tile of 128 keys against 0.75 for its bytes.)
 //
-// Warps: 0-7 softmax, 8 TMA producer of the codes, 9 issuer of the S MMAs, 10 of the PV MMAs, 11 ancestor masks and TMA
-// producer of Q, 12-15 expansion (Q: a thread has a row; V: a thread has a key; the tree's keys and values).  Every wait is
-// bounded; all threads reach the final barrier before tensor memory is freed.
+// Warps: 0-7 the queries' parts, then softmax; 8 TMA producer of the codes, 9 issuer of the S MMAs, 10 of the PV MMAs, 11
+// ancestor masks and TMA producer of Q, 12-15 expansion (V: a thread has a key; the tree's keys and values).  Every wait is bounded; all threads
+// reach the final barrier before tensor memory is freed.
 #include "core.cuh"
 #include "q8.cuh"
 #include "tmap.h"
@@ -42,7 +42,6 @@ struct Q8Maps {
 // this CTA has of a tile's keys, whole; one of V its columns of all 128 keys.
 template <int PAIR, int D>
 struct GeoQ8 {
-  static constexpr int kBlocks = D / 64;
   static constexpr int kQ = 128 * D;                                   // one part
   static constexpr int kVRow = PAIR == 2 ? 64 : D;                     // bytes of a key in a unit of V
   static constexpr int kVBlk = SPX_TILE_KEYS * 128, kVStage = kVBlk * (kVRow / 64);
@@ -54,59 +53,100 @@ struct GeoQ8 {
   static_assert(nv * kVStage >= 2 * kQ, "the V stages hold the bf16 queries in the beginning");
 };
 
-// Scales of a tile, per group of 32 keys.
-struct Q8Scales {
-  float k[4], v_log2[4], v_inv[4];
+// Scales of a tile, per group of 32 keys.  Those of all tiles of a run are made when it begins and lie behind the control block:
+// fetched by the softmax warps tile by tile they cost 600 cycles of every 3800, most of it for code that is out of the
+// instruction cache by the time it is needed again.
+struct alignas(16) Q8Scales {
+  float4 k, v_log2, v_inv;
 };
 struct CtrlQ8 {
   Ctrl c;                                      // (its K ring is not used; v_full, v_empty: the f16 stages)
   uint64_t k_full[kMaxUnits];                  // leader: one arrival per CTA (the producer's with its bytes, or the tree's)
   uint64_t k_empty[kMaxUnits];                 // each CTA: MMA completion
   uint64_t vc_full[kMaxUnits], vc_empty[kMaxUnits];      // this CTA: codes of V, between the producer and the expansion
-  uint64_t q_land;                             // this CTA: the bf16 queries have landed
+  uint64_t q_land, q_read;                     // this CTA: the bf16 queries have landed; 8 warps have read them
+  uint64_t q_ready;                            // leader: 8 warps per CTA have made their query rows
+  uint64_t sc_ready;                           // this CTA: the scales of the run's prefix tiles are in shared memory
   int tree_k[4], tree_v[4];                    // exponents of the tree's groups
   float q_scale[128];
 };
-constexpr int kCtrlBytesQ8 = 8192;
+constexpr int kCtrlBytesQ8 = 7168;
 static_assert(sizeof(CtrlQ8) <= kCtrlBytesQ8, "control block too large");
 template <int PAIR, int D>
 constexpr int smem_q8() {
-  return GeoQ8<PAIR, D>::kCtrl + kCtrlBytesQ8 + 1024;
+  return GeoQ8<PAIR, D>::kCtrl + kCtrlBytesQ8 + kSpxRunQ8 * (int)sizeof(Q8Scales) + 1024;
 }
 
-// A worker has one run of tiles of one problem.
-struct OneRun {
-  int n;
-  bool done;
-  __device__ __forceinline__ bool next() {
-    const bool first = !done;
-    done = true;
-    return first;
-  }
-};
-
-// ---- forms of the instructions for e4m3 and for a pair -----------------------------------------------------
+// ---- MMAs issued by a whole warp -----------------------------------------------------------------------------
+// All lanes come to the instruction, and it elects the one that issues it (the same one every time), so that the compiler knows
+// the operands to be the warp's and keeps them in uniform registers.  Issued by one thread of a diverged warp an MMA takes that
+// thread 133 cycles (188 with A in tensor memory), this way 64 to 77: as long as the tensor cores need for it.
 template <int PAIR>
 __device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
   if constexpr (PAIR == 2)
     asm volatile(
-        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+        "{\n\t.reg .pred p, e;\n\t.reg .b64 da, db;\n\t"
+        "elect.sync _|e, 0xffffffff;\n\t"
         "mov.b64 da, {%1, %3};\n\t"
         "mov.b64 db, {%2, %3};\n\t"
         "setp.ne.b32 p, %5, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], da, db, %4, p;\n\t}"
+        "@e tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], da, db, %4, p;\n\t}"
         ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
         : "memory");
   else
     asm volatile(
-        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+        "{\n\t.reg .pred p, e;\n\t.reg .b64 da, db;\n\t"
+        "elect.sync _|e, 0xffffffff;\n\t"
         "mov.b64 da, {%1, %3};\n\t"
         "mov.b64 db, {%2, %3};\n\t"
         "setp.ne.b32 p, %5, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %4, p;\n\t}"
+        "@e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %4, p;\n\t}"
         ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
         : "memory");
 }
+// f16, A in tensor memory.
+template <int PAIR>
+__device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t hi, uint32_t idesc,
+                                           uint32_t accumulate) {
+  if constexpr (PAIR == 2)
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t.reg .b64 db;\n\t"
+        "elect.sync _|e, 0xffffffff;\n\t"
+        "mov.b64 db, {%2, %3};\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "@e tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], db, %4, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t.reg .b64 db;\n\t"
+        "elect.sync _|e, 0xffffffff;\n\t"
+        "mov.b64 db, {%2, %3};\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+template <int PAIR>
+__device__ __forceinline__ void commit_warp(uint64_t* bar) {
+  if constexpr (PAIR == 2)
+    asm volatile(
+        "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}"
+        ::"r"(smem_u32(bar)), "h"((uint16_t)3)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
+        ::"r"(smem_u32(bar))
+        : "memory");
+}
+// A wait of the whole warp: true for all lanes or for none.
+__device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+  return __all_sync(0xffffffffu, wait_c(bar, parity, abort_flag));
+}
+
 // A warp's arrival on a barrier of the leader, behind its plain stores to shared memory that the pair's MMAs read.
 template <int PAIR>
 __device__ __forceinline__ void publish(uint64_t* bar, int lane) {
@@ -129,7 +169,7 @@ __device__ __forceinline__ int code_place(int row, int c) {
 // One key's codes (W of them) as f16 into a stage.
 template <int W>
 __device__ __forceinline__ void expand_key(const unsigned char* unit, unsigned char* stage, int key) {
-#pragma unroll
+#pragma unroll 1
   for (int c = 0; c < W / 16; c += 2) {
     uint4 x[2];
 #pragma unroll
@@ -152,15 +192,12 @@ __device__ __forceinline__ int e4m3_exponent(uint32_t amax) {
 __device__ __forceinline__ uint32_t amax_bf16x8(uint32_t m, uint4 x) {
   return amax_bf16x2(amax_bf16x2(amax_bf16x2(amax_bf16x2(m, x.x), x.y), x.z), x.w);
 }
-// High and low parts of four bf16 values times f.
+// High and low parts of four bf16 values times f.  As f16 the values are exact (8 bits, at most 2^8), and so is the difference.
 __device__ __forceinline__ void split4(uint32_t a, uint32_t b, float f, uint32_t& hi, uint32_t& lo) {
-  const float x0 = __uint_as_float(a << 16) * f, x1 = __uint_as_float(a & 0xffff0000u) * f;
-  const float x2 = __uint_as_float(b << 16) * f, x3 = __uint_as_float(b & 0xffff0000u) * f;
-  const uint32_t h0 = f32x2_to_e4m3x2(x0, x1), h1 = f32x2_to_e4m3x2(x2, x3);
-  const uint32_t w0 = e4m3x2_to_f16x2(h0), w1 = e4m3x2_to_f16x2(h1);
-  const float2 y0 = f16x2_to_f32x2(w0), y1 = f16x2_to_f32x2(w1);
+  const uint32_t x0 = bf16x2_to_f16x2(a, f), x1 = bf16x2_to_f16x2(b, f);
+  const uint32_t h0 = f16x2_to_e4m3x2(x0), h1 = f16x2_to_e4m3x2(x1);
   hi = h0 | (h1 << 16);
-  lo = f32x2_to_e4m3x2(x0 - y0.x, x1 - y0.y) | (f32x2_to_e4m3x2(x2 - y1.x, x3 - y1.y) << 16);
+  lo = f16x2_to_e4m3x2(sub_f16x2(x0, e4m3x2_to_f16x2(h0))) | (f16x2_to_e4m3x2(sub_f16x2(x1, e4m3x2_to_f16x2(h1))) << 16);
 }
 // 16 bf16 values (two 16-byte pieces) as a piece of high parts and one of low parts.
 __device__ __forceinline__ void split16(uint4 x, uint4 y, float f, unsigned char* hi, unsigned char* lo) {
@@ -183,25 +220,27 @@ __device__ __forceinline__ uint32_t tree_amax(const __nv_bfloat16* src, bool val
   return __reduce_max_sync(0xffffffffu, m);
 }
 
-// Issuer of the S MMAs.  has_tree: the last tile of the run is the tree's, two units of K.
+// Issuers of the S and of the PV MMAs (issue_s and issue_pv of core.cuh for one run of tiles, by whole warps of the leader CTA).
+// has_tree: the last tile of the run is the tree's, two units of K.
 template <int PAIR, int D>
 __device__ __forceinline__ bool issue_s_q8(CtrlQ8* ctl8, unsigned char* base, int n_tiles, bool has_tree, volatile int* abort_flag) {
   using G = GeoQ8<PAIR, D>;
   Ctrl* ctl = &ctl8->c;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, ctl->tmem_base, 0);
   constexpr uint32_t idesc = idesc_f32<true>(128 * PAIR, SPX_TILE_KEYS, false, false);     // (e4m3: type fields 0 as for f16)
   // rows of D bytes, 8-row groups of 8 D; 128-byte swizzle, or 64-byte (mode 4) for D = 64
   constexpr uint32_t hi = D == 128 ? desc_hi(1024) : ((512u >> 4) | (1u << 14) | (4u << 29));
   const uint32_t q_lo = desc_lo(smem_u32(base), 16), k_lo = desc_lo(smem_u32(base + G::k8_off), 16);
   int st = 0;
   uint32_t ph = 0;
-  bool ok = wait_c(&ctl->q_full, 0, abort_flag);
+  bool ok = wait_warp(&ctl8->q_ready, 0, abort_flag);
   for (int j = 0; j < n_tiles && ok; ++j) {
     const int w = j & 1, units = has_tree && j == n_tiles - 1 ? 2 : 1;
     // the rows of the tile before last are in registers: its S buffer is free
-    if (j >= kWG) ok = wait_c(&ctl->s_free[w], (j / kWG - 1) & 1, abort_flag);
-    const uint32_t d = ctl->tmem_base + kColS + w * 128;
+    if (j >= kWG) ok = wait_warp(&ctl->s_free[w], (j / kWG - 1) & 1, abort_flag);
+    const uint32_t d = tmem + kColS + w * 128;
     for (int u = 0; u < units && ok; ++u) {
-      ok = wait_c(&ctl8->k_full[st], ph, abort_flag);
+      ok = wait_warp(&ctl8->k_full[st], ph, abort_flag);
       if (!ok) break;
       tc_fence_after();
       const uint32_t kb = k_lo + st * (G::kKUnit >> 4);
@@ -210,21 +249,54 @@ __device__ __forceinline__ bool issue_s_q8(CtrlQ8* ctl8, unsigned char* base, in
 #pragma unroll
         for (int kk = 0; kk < D / 32; ++kk)
           mma_f8<PAIR>(d, q_lo + part * (G::kQ >> 4) + kk * 2, kb + kk * 2, hi, idesc, part + kk > 0 || u > 0 ? 1u : 0u);
-      commit<PAIR>(&ctl8->k_empty[st]);
+      commit_warp<PAIR>(&ctl8->k_empty[st]);
       if (++st == G::kKUnits) {
         st = 0;
         ph ^= 1;
       }
     }
-    if (ok) commit<PAIR>(&ctl->s_full[w]);
+    if (ok) commit_warp<PAIR>(&ctl->s_full[w]);
   }
-  commit<PAIR>(&ctl->drain);
+  commit_warp<PAIR>(&ctl->drain);
+  return ok;
+}
+template <int PAIR, int D>
+__device__ __forceinline__ bool issue_pv_q8(CtrlQ8* ctl8, unsigned char* base, int n_tiles, volatile int* abort_flag) {
+  using G = GeoQ8<PAIR, D>;
+  Ctrl* ctl = &ctl8->c;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, ctl->tmem_base, 0);
+  constexpr uint32_t idesc = idesc_f32<true>(128 * PAIR, D, false, true), hi = desc_hi(1024);
+  const uint32_t v_lo = desc_lo(smem_u32(base + G::v_off), PAIR == 2 ? 16 : G::kVBlk);
+  int st = 0;
+  uint32_t ph = 0;
+  bool ok = true;
+  for (int j = 0; j < n_tiles && ok; ++j) {
+    const int w = j & 1;
+    ok = wait_warp(&ctl->v_full[st], ph, abort_flag) && wait_warp(&ctl->p_full[w], (j / kWG) & 1, abort_flag);
+    if (!ok) break;
+    tc_fence_after();
+    const uint32_t vb = v_lo + st * (G::kVStage >> 4), pa = tmem + kColP + w * 64;
+#pragma unroll
+    for (int kk = 0; kk < SPX_TILE_KEYS / 16; ++kk)
+      mma_f16_ts<PAIR>(tmem + kColO, pa + kk * 8, vb + kk * 128, hi, idesc, kk > 0 || j > 0 ? 1u : 0u);
+    commit_warp<PAIR>(&ctl->pv_done[w]);
+    commit_warp<PAIR>(&ctl->v_empty[st]);
+    if (++st == G::nv) {
+      st = 0;
+      ph ^= 1;
+    }
+  }
+  if (ok) commit_warp<PAIR>(&ctl->o_done);
+  // everything issued by both must be complete before tensor memory is released
+  commit_warp<PAIR>(&ctl->drain);
+  for (int spin = 0; spin < (1 << 22) && !mbar_test_wait(&ctl->drain, 0); ++spin) {}
+  __syncwarp();
   return ok;
 }
 
 // softmax_tile of core.cuh with scales: `mult` is the row's factor (softmax scale, log2 e, the power of two of the query row).
 template <int D, class MaskFn, class SumFn>
-__device__ __forceinline__ bool softmax_tile_q8(const RowCtx& rc, const Q8Scales& sc, float mult, uint32_t t, bool need_mask,
+__device__ __forceinline__ bool softmax_tile_q8(const RowCtx& rc, const Q8Scales* scales, float mult, uint32_t t, bool need_mask,
                                                 MaskFn&& mask, SumFn&& sums, float& m_loc, float& l) {
   Ctrl* ctl = rc.ctl;
   const int w = rc.w, wp = w ^ 1;
@@ -237,6 +309,7 @@ __device__ __forceinline__ bool softmax_tile_q8(const RowCtx& rc, const Q8Scales
   tmem_ld32(s_addr + 32, s1);
   tmem_ld32(s_addr + 64, s2);
   tmem_ld32(s_addr + 96, s3);
+  const float4 ks = scales->k, ev = scales->v_log2;
   float m_cur = -INFINITY;
   if (!first) {
     if (!mbar_wait(&ctl->m_pub[wp], ((t - 1) / kWG) & 1, rc.abort_flag)) return false;
@@ -262,9 +335,9 @@ __device__ __forceinline__ bool softmax_tile_q8(const RowCtx& rc, const Q8Scales
     }
     return fmaxf(a, b);
   };
-  const float f0 = mult * sc.k[0], f1 = mult * sc.k[1], f2 = mult * sc.k[2], f3 = mult * sc.k[3];
-  const float m_tile = fmaxf(fmaxf(fmaf(max_group(s0), f0, sc.v_log2[0]), fmaf(max_group(s1), f1, sc.v_log2[1])),
-                             fmaxf(fmaf(max_group(s2), f2, sc.v_log2[2]), fmaf(max_group(s3), f3, sc.v_log2[3]))) - kHeadroom;
+  const float f0 = mult * ks.x, f1 = mult * ks.y, f2 = mult * ks.z, f3 = mult * ks.w;
+  const float m_tile = fmaxf(fmaxf(fmaf(max_group(s0), f0, ev.x), fmaf(max_group(s1), f1, ev.y)),
+                             fmaxf(fmaf(max_group(s2), f2, ev.z), fmaf(max_group(s3), f3, ev.w))) - kHeadroom;
 
   float m_new = m_cur;
   bool rescale = false;
@@ -319,7 +392,7 @@ __device__ __forceinline__ bool softmax_tile_q8(const RowCtx& rc, const Q8Scales
     float gs0, gs1, gs2, gs3;
     unpack_f32x2(acc01, gs0, gs1);
     unpack_f32x2(acc23, gs2, gs3);
-    const float inv = sc.v_inv[c], gs = ((gs0 + gs1) + (gs2 + gs3)) * inv;
+    const float inv = reinterpret_cast<const float*>(&scales->v_inv)[c], gs = ((gs0 + gs1) + (gs2 + gs3)) * inv;
     l += gs;
     sums(c, v, gs, inv);
     uint32_t pk[16];
@@ -327,10 +400,10 @@ __device__ __forceinline__ bool softmax_tile_q8(const RowCtx& rc, const Q8Scales
     for (int k = 0; k < 16; ++k) pk[k] = pack_f16x2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1]));
     tmem_st16(p_addr + c * 16, pk);
   };
-  exp_chunk(s0, 0, f0, sc.v_log2[0] - m_new);
-  exp_chunk(s1, 1, f1, sc.v_log2[1] - m_new);
-  exp_chunk(s2, 2, f2, sc.v_log2[2] - m_new);
-  exp_chunk(s3, 3, f3, sc.v_log2[3] - m_new);
+  exp_chunk(s0, 0, f0, ev.x - m_new);
+  exp_chunk(s1, 1, f1, ev.y - m_new);
+  exp_chunk(s2, 2, f2, ev.z - m_new);
+  exp_chunk(s3, 3, f3, ev.w - m_new);
   tmem_wait_st();
   tc_fence_before();
   warp_arrive_cluster(rc.p_full, rc.lane);
@@ -349,9 +422,9 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
                                                          ~static_cast<uintptr_t>(1023));
   CtrlQ8* ctl8 = reinterpret_cast<CtrlQ8*>(base + G::kCtrl);
   Ctrl* ctl = &ctl8->c;
+  Q8Scales* scales = reinterpret_cast<Q8Scales*>(base + G::kCtrl + kCtrlBytesQ8);
   volatile int* abort_flag = &ctl->abort_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const G geo;
 
   const int rank = PAIR == 2 ? (int)cluster_rank() : 0;
   const int worker = blockIdx.x / PAIR, prob = worker / p.cpp;
@@ -367,43 +440,48 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
       mbar_init(&ctl8->vc_empty[lane], 4);
     } else if (lane == kMaxUnits) {
       mbar_init(&ctl8->q_land, 1);
+      mbar_init(&ctl8->q_read, 8);
+      mbar_init(&ctl8->sc_ready, 4);
+      mbar_init(&ctl8->q_ready, 8 * PAIR);
     }
     fence_mbar_init();
   }
   setup<PAIR, false, 4>(ctl, warp, lane);
   pdl_launch_dependents();
   bool ok = true;
-  OneRun work{n_tiles, false};
 
   if (warp >= kExpandWarp) {
-    // ================================ queries, V and the tree in the tensor cores' types ======
+    // ================================ V and the tree in the tensor cores' types ================
     setmaxnreg_dec<kRegsOtherQ8>();
     const int group = warp - kExpandWarp, key = group * 32 + lane;
     pdl_wait();
-    ok = mbar_wait(&ctl8->q_land, 0, abort_flag);
-    if (ok) {
-      const unsigned char* q = base + G::v_off;          // (bf16, where V's stages will be)
-      uint32_t m = 0u;
-#pragma unroll 4
-      for (int c = 0; c < D / 8; ++c) m = amax_bf16x8(m, *reinterpret_cast<const uint4*>(q + f16_place(key, c)));
-      const int e = e4m3_exponent(m);
-      const float f = exp2_int(-e);
-#pragma unroll 2
-      for (int c = 0; c < D / 16; ++c)
-        split16(*reinterpret_cast<const uint4*>(q + f16_place(key, 2 * c)), *reinterpret_cast<const uint4*>(q + f16_place(key, 2 * c + 1)),
-                f, base + code_place<D>(key, c), base + G::kQ + code_place<D>(key, c));
-      ctl8->q_scale[key] = exp2_int(e);
-      publish<PAIR>(&ctl->q_full, lane);
+    // scales of the run: a thread has a group of a tile (groups behind the prefix have no key and any scale)
+    for (int i = key; i < n_pref * 4; i += 128) {
+      const int token = min((tile_lo + (i >> 2)) * SPX_TILE_KEYS + (i & 3) * 32, p.L - 1);
+      const long long at = (long long)(token >> args.log_block) * args.s_sb + (long long)g * args.s_sh;
+      const uint32_t kc = args.Ks[at], vcode = args.Vs[at];
+      Q8Scales* sc = scales + (i >> 2);
+      reinterpret_cast<float*>(&sc->k)[i & 3] = e8m0_value(kc);
+      reinterpret_cast<float*>(&sc->v_log2)[i & 3] = e8m0_log2(vcode);
+      reinterpret_cast<float*>(&sc->v_inv)[i & 3] = e8m0_value(vcode == 255u ? 255u : 254u - vcode);
     }
-    named_bar_sync(1, 128);                              // everybody has read the bf16 queries
+    warp_arrive(&ctl8->sc_ready, lane);
+    ok = mbar_wait(&ctl8->q_read, 0, abort_flag);        // (they lie where V's stages will be)
     int vc = 0, vst = 0;
     uint32_t vcph = 0, vph = 1;
     for (int j = 0; j < n_pref && ok; ++j) {
       ok = mbar_wait(&ctl8->vc_full[vc], vcph, abort_flag) && wait_c(&ctl->v_empty[vst], vph, abort_flag);
       if (!ok) break;
       expand_key<G::kVRow>(base + G::v8_off + vc * G::kVUnit, base + G::v_off + vst * G::kVStage, key);
-      publish<PAIR>(&ctl->v_full[vst], lane);
-      if (lane == 0) mbar_arrive(&ctl8->vc_empty[vc]);
+      // The stores are read by the tensor cores of this SM alone, and the proxy fence has them in place for those; what the arrival
+      // tells the leader, which may be the other CTA, is only that.  (Releasing at the cluster's scope takes 1100 to 1900 cycles,
+      // longer than a tile.)
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) {
+        arrive_cluster(leader_addr<PAIR>(&ctl->v_full[vst]));
+        mbar_arrive(&ctl8->vc_empty[vc]);
+      }
       if (++vc == G::kVUnits) {
         vc = 0;
         vcph ^= 1;
@@ -422,8 +500,13 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
         const bool node = key < p.T;
         const uint32_t km = tree_amax<D>(kt + (long long)key * a.tkv_st, node), vm = tree_amax<D>(vt + (long long)key * a.tkv_st, node);
         if (lane == 0) {
-          ctl8->tree_k[group] = e4m3_exponent(km);
-          ctl8->tree_v[group] = f16_exponent(vm);
+          const int ke = e4m3_exponent(km), ve = f16_exponent(vm);
+          ctl8->tree_k[group] = ke;
+          ctl8->tree_v[group] = ve;
+          Q8Scales* sc = scales + n_pref;                // (read once the tile's scores are there)
+          reinterpret_cast<float*>(&sc->k)[group] = exp2_int(ke);
+          reinterpret_cast<float*>(&sc->v_log2)[group] = (float)ve;
+          reinterpret_cast<float*>(&sc->v_inv)[group] = exp2_int(-ve);
         }
       }
       named_bar_sync(1, 128);
@@ -500,7 +583,7 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
   } else if (warp == kMmaWarp) {
     setmaxnreg_dec<kRegsOtherQ8>();
     pdl_wait();                                          // (a bounded wait must not count the time of the kernel before)
-    if (lane == 0 && rank == 0) ok = issue_s_q8<PAIR, D>(ctl8, base, n_tiles, has_tree, abort_flag);
+    if (rank == 0) ok = issue_s_q8<PAIR, D>(ctl8, base, n_tiles, has_tree, abort_flag);
   } else if (warp == kPvWarp) {
     setmaxnreg_dec<kRegsOtherQ8>();
     if (lane == 0) {
@@ -511,16 +594,17 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
       }
     }
     pdl_wait();
-    if (lane == 0 && rank == 0) ok = issue_pv<PAIR, D, true>(ctl, base, geo, work, abort_flag);
+    __syncwarp();
+    if (rank == 0) ok = issue_pv_q8<PAIR, D>(ctl8, base, n_tiles, abort_flag);
   } else if (warp == kTreeWarp) {
     // ================================ ancestor masks, TMA producer of Q =======================
     setmaxnreg_dec<kRegsOtherQ8>();
     pdl_wait();
     if (lane == 0) {
       const uint32_t bar = smem_u32(&ctl8->q_land);
-      arrive_expect_tx_cluster(bar, 128 * 128 * G::kBlocks);
+      arrive_expect_tx_cluster(bar, 2 * G::kQ);
 #pragma unroll
-      for (int ds = 0; ds < G::kBlocks; ++ds)
+      for (int ds = 0; ds < D / 64; ++ds)
         tma_load<1>(smem_u32(base + G::v_off + ds * 128 * 128), &maps.q, bar, 64 * ds, g * p.G, (rblk * p.RB + rank * 128) / p.G);
     }
     __syncwarp();
@@ -565,14 +649,30 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
       tmem_wait_st();
       tc_fence_before();
     }
-    // Scales of a tile: lane c has that of K's group c, lane 4 + c of V's, fetched two tiles ahead.
-    const uint8_t* s_src = (lane & 4 ? args.Vs : args.Ks) + (long long)g * args.s_sh;
-    auto scale_of = [&](int j) -> uint32_t {
-      const int token = (tile_lo + j) * SPX_TILE_KEYS + (lane & 3) * 32;
-      return lane < 8 && j < n_pref && token < p.L ? s_src[(long long)(token >> args.log_block) * args.s_sb] : 127u;
-    };
     pdl_wait();
-    uint32_t codes = scale_of(rc.w);
+    {
+      // Query rows, 16 a warp and two lanes a row: their high and low parts, and the power of two.  The loops stay loops: this
+      // runs once, and instructions that are not in the cache yet are what it waits for.  (All unrolled, rows in registers
+      // straight from memory, it took 5000 to 7000 cycles, with everybody waiting; four warps in loops 5000.)
+      const int row = warp * 16 + (lane >> 1), half = lane & 1;
+      const unsigned char* q = base + G::v_off;            // (bf16, where V's stages will be)
+      uint32_t m = 0u;
+      ok = mbar_wait(&ctl8->q_land, 0, abort_flag);
+      if (ok) {
+#pragma unroll 2
+        for (int c = half * (D / 16); c < (half + 1) * (D / 16); ++c) m = amax_bf16x8(m, *reinterpret_cast<const uint4*>(q + f16_place(row, c)));
+        m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+        const int e = e4m3_exponent(m);
+        const float f = exp2_int(-e);
+#pragma unroll 1
+        for (int c = half * (D / 32); c < (half + 1) * (D / 32); ++c)
+          split16(*reinterpret_cast<const uint4*>(q + f16_place(row, 2 * c)), *reinterpret_cast<const uint4*>(q + f16_place(row, 2 * c + 1)),
+                  f, base + code_place<D>(row, c), base + G::kQ + code_place<D>(row, c));
+        if (half == 0) ctl8->q_scale[row] = exp2_int(e);
+      }
+      warp_arrive(&ctl8->q_read, lane);
+      publish<PAIR>(&ctl8->q_ready, lane);
+    }
     const int t_node = valid ? r / p.G : 0;
     float m_loc = -INFINITY, l = 0.f, mult = 0.f;
     bool known = false;                                  // mult is the row's
@@ -584,24 +684,14 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
       const int tile = tile_lo + j;
       const bool is_tree = tile == p.TPH;
       const int nkeys = is_tree ? p.T : min(SPX_TILE_KEYS, p.L - tile * SPX_TILE_KEYS);
-      const uint32_t codes_next = scale_of(j + kWG);
       if (!known || is_tree) {
         // (the scores are there, so the query rows and the tree's scales are)
-        ok = mbar_wait(&ctl->s_full[rc.w], (j / kWG) & 1, abort_flag);
+        ok = mbar_wait(&ctl->s_full[rc.w], (j / kWG) & 1, abort_flag) && mbar_wait(&ctl8->sc_ready, 0, abort_flag);
         if (ok && is_tree) ok = mbar_wait(&ctl->anc_ready, 0, abort_flag);
         if (!ok) break;
         mult = p.scale2 * ctl8->q_scale[rc.row_t];
         known = true;
       }
-      Q8Scales sc;
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const uint32_t kc = __shfl_sync(0xffffffffu, codes, c), vcode = __shfl_sync(0xffffffffu, codes, 4 + c);
-        sc.k[c] = is_tree ? exp2_int(ctl8->tree_k[c]) : e8m0_value(kc);
-        sc.v_log2[c] = is_tree ? (float)ctl8->tree_v[c] : e8m0_log2(vcode);
-        sc.v_inv[c] = is_tree ? exp2_int(-ctl8->tree_v[c]) : e8m0_value(vcode == 255u ? 255u : 254u - vcode);
-      }
-      codes = codes_next;
       float cg[4];                                       // sums of the tile's four groups of 32 keys
       float* mass = nullptr;
       long long rowbase = 0;
@@ -610,7 +700,7 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
         mass = a.ws + p.off_mass + rowbase * p.CPT;
       }
       ok = softmax_tile_q8<D>(
-          rc, sc, mult, j, is_tree || nkeys < SPX_TILE_KEYS,
+          rc, scales + j, mult, j, is_tree || nkeys < SPX_TILE_KEYS,
           [&](unsigned long long& lo, unsigned long long& hi) {
             if (is_tree) {                 // this node and its ancestors (a padding row sees key 0)
               lo = valid ? ctl->anc[t_node][0] : 1ull;
