@@ -299,39 +299,69 @@ void lay_out_rows_workspace(AttnPlan* plan, int cluster) {
   lay_out_workspace(plan);
 }
 
-// Few rows (rows_q8.cu): units are groups of 16 keys, prefix and tree alike.
+// The largest cluster of which one per problem is resident at once (at most `most`), or 0.
+int rows_q8_cluster(int problems, int most) {
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return 0;
+  }
+  for (int s = most < 16 ? most : 16; s >= 1; --s)
+    if (problems <= spx_rows_q8_max_clusters(dev, s)) return s;
+  return 0;
+}
+
+// Few rows (rows_q8.cu): units are groups of 16 keys, prefix and tree alike; row blocks of 8 or 16.
 int lay_out_rows_q8(AttnPlan* plan) {
   AttnPlan& p = *plan;
   p.kernel = 5;
-  p.RB = p.q_rows = kSpxRowsQ8;
-  p.n_rblk = 1;
-  p.NP = p.Hkv;
+  p.RB = 32;                                               // (of the partial results, as the merge kernel takes them)
+  p.q_rows = p.rows <= 8 ? 8 : 16;
+  p.n_rblk = (p.rows + p.q_rows - 1) / p.q_rows;
+  p.NP = p.Hkv * p.n_rblk;
   p.TPH = (p.L + 15) / 16;
   p.UPP = p.TPH + (p.T + 15) / 16;
   if ((long long)p.NP * p.UPP > (1ll << 30)) return SPECEXT_ERR_UNSUPPORTED;
   p.U = p.NP * p.UPP;
-  p.cpp = sm_count() / p.NP;
-  if (p.cpp > (p.UPP + 7) / 8) p.cpp = (p.UPP + 7) / 8;
-  if (p.cpp < 1) p.cpp = 1;
-  int dev = -1, size = 0;
-  if (cudaGetDevice(&dev) == cudaSuccess) {
-    for (int s = 16; s >= 1 && size == 0; --s)
-      if (s <= p.cpp && p.NP <= spx_rows_q8_max_clusters(dev, s)) size = s;
-  } else {
-    (void)cudaGetLastError();
+  const int full = (p.UPP + 7) / 8;                        // CTAs that find a unit for each of their warps
+  const int size = rows_q8_cluster(p.NP, full);
+  if (p.n_rblk > 1) {                                      // (only in clusters: rows_instead has seen to it)
+    lay_out_rows_workspace(&p, size > 0 ? size : 1);
+    return SPECEXT_OK;
   }
+  p.cpp = sm_count() / p.NP;
+  if (p.cpp > full) p.cpp = full;
+  if (p.cpp < 1) p.cpp = 1;
   lay_out_rows_workspace(&p, 0);
   const long long split_floats = p.total_floats;           // (the workspace does not depend on what clusters the device holds)
   // The clusters merge among themselves, which saves 1.5 to 3 us with the second launch, but they leave SMs idle (eight of ten CTAs
   // are all that fit at once), so that a warp takes more steps of 16 keys.  us per call, replayed, split / cluster (steps): 32
   // query / 8 KV heads, one node: 1K 6.9 / 5.1, 16K 12.9 / 12.1 (8 / 13), 128K 48.4 / 48.4 (57 / 103: HBM either way); 16 / 2 heads:
   // 4K 9.2 / 5.7, 32K 14.5 / 12.8 (4 / 17), 128K 21.9 / 37.9 (14 / 65); 12 x 64 heads: 16K 11.3 / 10.8 (11 / 15), 64K 27.7 / 30.9
-  // (43 / 57).  More than 8 rows make a step longer: 16 rows at 8K 11.8 / 10.9 (4 / 7), 16K 15.0 / 15.2 (8 / 13); 32 rows at
-  // 8K 20.5 / 18.7, 16K 27.0 / 29.1.
+  // (43 / 57).  More than 8 rows make a step longer: 16 rows at 8K 11.8 / 10.9 (4 / 7), 16K 15.0 / 15.2 (8 / 13).
   const int split_steps = (p.UPP + 8 * p.cpp - 1) / (8 * p.cpp), steps = size > 0 ? (p.UPP + 8 * size - 1) / (8 * size) : 0;
   if (size > 0 && steps - split_steps <= (p.rows <= 8 ? 13 : 4)) lay_out_rows_workspace(&p, size);
   if (p.total_floats < split_floats) p.total_floats = split_floats;
   return SPECEXT_OK;
+}
+
+// Whether the kernel for few rows takes a call (p: sizes and the plan of the other one).  Up to 16 rows always.  More go there in
+// blocks of 16, each a cluster, which read the same keys again and again: as long as a warp has few steps of 128 keys of its
+// CTA, about 0.68 us each on top of 7, against 1.0 us a tile (0.7 with head_dim 64) on top of 14 (12.5).  us per call, replayed,
+// this kernel / the other (steps, tiles): 60 nodes of 32 query / 8 KV heads 1K 15.8 / 17.2 (9, 1), 2K 20.6 / 17.2 (17, 2); 16 nodes 2K
+// 10.0 / 16.9 (5, 1), 8K 18.0 / 19.0 (17, 4); 10 nodes of 16 / 2 heads 4K 9.6 / 17.8 (4, 1), 16K 15.5 / 22.6 (13, 2); 5 nodes of
+// 32 / 8 16K 21.4 / 23.5 (19, 8), 12 nodes 24.4 / 24.0 (26, 8); 60 nodes of 32 KV heads 1K 16.1 / 17.7 (9, 3), 4K 32.8 / 25.0
+// (33, 9), 20 nodes 8K 30.0 / 31.6 (33, 17); 12 x 64 heads, 60 nodes 1K 10.5 / 14.0 (3, 1), 4K 16.2 / 14.8 (11, 3).  (Blocks of 32
+// rows: 16 nodes 2K 14.0, 10 nodes of 16 / 2 heads 4K 13.0: a step of 32 rows spills and takes more than twice as long.)
+bool rows_instead(const AttnPlan& p) {
+  if (p.want_score) return false;
+  if (p.rows <= 16) return true;
+  const int problems = p.Hkv * ((p.rows + 15) / 16), units = (p.L + 15) / 16 + (p.T + 15) / 16;
+  if (problems > sm_count()) return false;
+  const int size = rows_q8_cluster(problems, (units + 7) / 8);
+  if (size == 0) return false;
+  const int steps = (units + 8 * size - 1) / (8 * size), tiles = (p.UPP + p.cpp - 1) / p.cpp;
+  return p.D == 64 ? 2 * steps <= 13 + 2 * tiles : 2 * steps <= 20 + 3 * tiles;
 }
 
 // The plan of an attention call on the 8-bit cache: every problem has the same whole number of workers.
@@ -342,10 +372,6 @@ int build_plan_q8(const specext_attn_desc* d, const specext_q8_desc* q, AttnPlan
   if (!q || block_log2(q->block_tokens) == 0) return q ? SPECEXT_ERR_UNSUPPORTED : SPECEXT_ERR_INVALID_ARG;
   if (!q8_strides(d->kv_stride_l, d->kv_stride_h, d->head_dim) || q->scale_stride_b < 1 || q->scale_stride_h < 1)
     return SPECEXT_ERR_INVALID_ARG;
-  if (p.rows <= kSpxRowsQ8 && !p.want_score) {
-    *out = p;
-    return lay_out_rows_q8(out);
-  }
   // one CTA on 128-row blocks, or pairs of CTAs on 256-row blocks for head_dim 128 and more than 128 rows
   const bool pair = p.D == 128 && p.rows > 128;
   p.kernel = 4;
@@ -364,6 +390,13 @@ int build_plan_q8(const specext_attn_desc* d, const specext_q8_desc* q, AttnPlan
   p.rem = p.UPP % p.cpp;
   p.max_segs = p.cpp;
   lay_out_workspace(&p);
+  if (rows_instead(p)) {
+    // (several row blocks need no workspace, but its size does not depend on what clusters the device holds)
+    const long long floats = p.rows > 16 ? p.total_floats : 0;
+    const int rows_rc = lay_out_rows_q8(&p);
+    if (rows_rc != SPECEXT_OK) return rows_rc;
+    if (p.total_floats < floats) p.total_floats = floats;
+  }
   *out = p;
   return SPECEXT_OK;
 }

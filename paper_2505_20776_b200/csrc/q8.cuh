@@ -77,8 +77,7 @@ __device__ __forceinline__ float2 f16x2_to_f32x2(uint32_t x) { return __half22fl
 
 constexpr int kSpxRunQ8 = 144;                      // tiles of a worker's run (their scales are kept in shared memory)
 cudaError_t spx_launch_verify_q8(const Q8Args& q, cudaStream_t st, int* n_launches);      // any rows, chunk sums
-cudaError_t spx_launch_rows_q8(const Q8Args& q, cudaStream_t st, int* n_launches);        // up to kSpxRowsQ8 rows, no chunk sums
-constexpr int kSpxRowsQ8 = 32;
+cudaError_t spx_launch_rows_q8(const Q8Args& q, cudaStream_t st, int* n_launches);        // row blocks of 8 or 16, no chunk sums
 int spx_rows_q8_max_clusters(int dev, int size);
 
 #endif  // SPECEXT_Q8_CUH_

@@ -1,5 +1,5 @@
-// Attention over the 8-bit prefix cache (q8.cuh) for few rows: single-token decoding, and trees of a few nodes, up to 32 stacked
-// (query head x node) rows of a KV head.  Here a key costs its bytes and next to nothing else, so the kernel is laid out to keep
+// Attention over the 8-bit prefix cache (q8.cuh) for few stacked (query head x node) rows of a KV head, single-token decoding first
+// of all, in blocks of 8 or 16, and for more where the prefix is short (the line is drawn at rows_instead in api.cu).  Here a key costs its bytes and next to nothing else, so the kernel is laid out to keep
 // loads in flight and to have no meeting points: keys are dealt in groups of 16, every warp has groups of its own (every eighth
 // of its CTA's) and a ring of its own in shared memory, which it fills by asynchronous copies five groups ahead, 160 KB in flight
 // per SM.  Nothing waits on a barrier before the end, there are no tensor maps to encode and to fetch, and the keys are dealt to
@@ -26,22 +26,21 @@ using namespace pair;
 namespace {
 
 constexpr int kGroupKeys = 16;
-constexpr int kMaxCluster = 16, kParts = 48;             // parts a CTA receives: CTAs x rows of its share (32 rows over 2 to 16)
+constexpr int kMaxCluster = 16, kParts = 30;             // parts a CTA receives: CTAs x rows of its share (16 rows over 1 to 16)
 constexpr float kHeadroom = 6.0f, kSlack = 8.0f;         // log2, see verify_q8.cu
 constexpr float kLn2 = 0.693147180559945309417f;
 
 // Shared memory: a ring per warp (a stage: 16 keys, then their values), whose room later holds the warps' O | parts received
-// from the cluster | queries, where they do not fit the registers.
+// from the cluster.
 template <int D, int NR>
 struct Geo {
   static constexpr int kWarps = 8, kThreads = kWarps * 32;
-  static constexpr bool kQueriesInSmem = NR == 4 && D == 128;
   static constexpr int kHalf = kGroupKeys * D, kStage = 2 * kHalf;
-  static constexpr int kStages = (D == 128 ? (NR == 4 ? 5 : 6) : 8) * 8 / kWarps;
+  static constexpr int kStages = D == 128 ? 6 : 8;
   static constexpr int kRing = kStages * kStage;
-  static constexpr int kRoom = kWarps * (kRing > NR * 8 * D * 4 ? kRing : NR * 8 * D * 4);
-  static constexpr int kParts0 = kRoom, kQueries0 = kParts0 + kParts * (D * 4 + 8);
-  static constexpr int kBytes = kQueries0 + (kQueriesInSmem ? NR * (D / 16) * 32 * 8 : 0) + 128;
+  static constexpr int kParts0 = kWarps * kRing;
+  static constexpr int kBytes = kParts0 + kParts * (D * 4 + 8) + 128;
+  static_assert(kRing >= NR * 8 * D * 4, "the rings later hold the warps' O");
   static_assert(kBytes + kWarps * 32 * 8 <= 232448, "more shared memory than a CTA can have");
 };
 
@@ -79,14 +78,7 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
 // What a warp has of its rows: lane (g, t) = (lane / 4, lane % 4).  S^T of a step: keys g and g + 8, rows 2t and 2t + 1 of a group.
 template <int D, int NR>
 struct WarpState {
-  static constexpr bool kInSmem = Geo<D, NR>::kQueriesInSmem;
-  // B operands: row g, elements (D/4) t + 4 j + {0, 1}, + {2, 3}; in registers, or [n][j][lane] in shared memory
-  uint32_t q[kInSmem ? 1 : NR][D / 16][2];
-  const uint2* q_smem;
-  __device__ __forceinline__ uint2 query(int n, int j) const {
-    if constexpr (kInSmem) return q_smem[(n * (D / 16) + j) * 32];
-    else return make_uint2(q[n][j][0], q[n][j][1]);
-  }
+  uint32_t q[NR][D / 16][2];                    // B operands: row g, elements (D/4) t + 4 j + {0, 1}, + {2, 3}
   float mult[NR][2];                            // of rows 2t, 2t + 1: softmax scale, log2 e, the query row's power of two
   float m[NR][2], l[NR][2];
   float o[D / 16][NR][4];                       // O^T: see store_o
@@ -107,10 +99,7 @@ __device__ __forceinline__ void step(WarpState<D, NR>& st, float k_scale, float 
     uint32_t a[4];
     k_frag(j, a);
 #pragma unroll
-    for (int n = 0; n < NR; ++n) {
-      const uint2 q = st.query(n, j);
-      mma16816(j & 1 ? s2[n] : s[n], a, q.x, q.y);
-    }
+    for (int n = 0; n < NR; ++n) mma16816(j & 1 ? s2[n] : s[n], a, st.q[n][j][0], st.q[n][j][1]);
   }
   bool high = false;
 #pragma unroll
@@ -220,10 +209,9 @@ __device__ __forceinline__ void staged_step(WarpState<D, NR>& st, const unsigned
       [&](int, int, int h) { return g + 8 * h < nkeys; });
 }
 
-// 16 tree nodes from `node0` on, bf16 from global memory; `anc`: ancestor masks, lane i has node i's.
+// 16 tree nodes from `node0` on, bf16 from global memory; lane i has in `row_seen` which of them row i sees.
 template <int D, int NR>
-__device__ __forceinline__ void tree_step(WarpState<D, NR>& st, const AttnArgs& a, int head, int node0, int row0, int log_g, uint32_t anc,
-                                          int lane) {
+__device__ __forceinline__ void tree_step(WarpState<D, NR>& st, const AttnArgs& a, int head, int node0, uint32_t row_seen, int lane) {
   const int g = lane >> 2, t = lane & 3, T = a.plan.T;
   uint32_t kw[2][D / 8], vw[4][D / 16];         // bf16 pairs
   uint32_t km = 0u, vm = 0u;
@@ -256,11 +244,7 @@ __device__ __forceinline__ void tree_step(WarpState<D, NR>& st, const AttnArgs& 
 #pragma unroll
   for (int n = 0; n < NR; ++n)
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const int node = (row0 + n * 8 + 2 * t + c) >> log_g;
-      const uint32_t mask = __shfl_sync(0xffffffffu, anc, node & 31);
-      seen[n][c] = node < T ? mask : 0u;
-    }
+    for (int c = 0; c < 2; ++c) seen[n][c] = __shfl_sync(0xffffffffu, row_seen, n * 8 + 2 * t + c);
   step<D, NR>(
       st, exp2_int(ke), (float)ve, exp2_int(-ve), true,
       [&](int j, uint32_t (&x)[4]) {
@@ -281,7 +265,7 @@ __device__ __forceinline__ void tree_step(WarpState<D, NR>& st, const AttnArgs& 
           x[i][3] = bf16x2_to_f16x2(o1, vf);
         }
       },
-      [&](int n, int c, int h) { return ((seen[n][c] >> (node0 + g + 8 * h)) & 1u) != 0; });
+      [&](int n, int c, int h) { return ((seen[n][c] >> (g + 8 * h)) & 1u) != 0; });
 }
 
 // The warps' results of one row's four columns: reference maximum, row sum, O.
@@ -321,15 +305,16 @@ rows_q8_kernel(const __grid_constant__ Q8Args args) {
   unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 127) & ~static_cast<uintptr_t>(127));
   __shared__ float2 warp_ml[kWarps][32];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-  const int worker = blockIdx.x, head = worker / p.cpp;
+  const int worker = blockIdx.x, prob = worker / p.cpp, head = prob / p.n_rblk;
+  const int row0 = (prob - head * p.n_rblk) * kRows;     // the problem's rows (with one row block: all)
   // units are groups of 16 keys; those from p.TPH on are the tree's
   const int unit_lo = spx_unit_start(p, worker), unit_hi = spx_unit_start(p, worker + 1);
-  const int first = unit_lo - head * p.UPP + warp, end = unit_hi - head * p.UPP, staged_end = min(end, p.TPH);
+  const int first = unit_lo - prob * p.UPP + warp, end = unit_hi - prob * p.UPP, staged_end = min(end, p.TPH);
   const int log_g = 31 - __clz(p.G);
   const uint32_t ring = smem_u32(base) + warp * G::kRing;
   const unsigned char* ring_ptr = base + warp * G::kRing;
   // CTAs of the cluster, rows of a CTA's share, and this one's
-  const int n_rows = p.rows, cs = CLUSTER ? p.cluster : 1, rank = CLUSTER ? (int)cluster_rank() : 0;
+  const int n_rows = min(kRows, p.rows - row0), cs = CLUSTER ? p.cluster : 1, rank = CLUSTER ? (int)cluster_rank() : 0;
   const int run = (n_rows + cs - 1) / cs, n_mine = min(run, n_rows - rank * run);
   __shared__ uint64_t arrived;                           // the parts of this CTA's rows, from all CTAs
   __shared__ int abort_flag;
@@ -405,11 +390,11 @@ rows_q8_kernel(const __grid_constant__ Q8Args args) {
   uint4 q_raw[NR][D / 32];
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
-    const int r = n * 8 + g;
+    const int r = row0 + n * 8 + g;
     const uint4* src = reinterpret_cast<const uint4*>(a.Q + (long long)(r >> log_g) * a.q_st +
                                                       (long long)(head * p.G + (r & (p.G - 1))) * a.q_sh + (D / 4) * t);
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) q_raw[n][i] = r < n_rows ? src[i] : make_uint4(0u, 0u, 0u, 0u);
+    for (int i = 0; i < D / 32; ++i) q_raw[n][i] = r < p.rows ? src[i] : make_uint4(0u, 0u, 0u, 0u);
   }
 #pragma unroll
   for (int i = 0; i < G::kStages - 1; ++i) request(first + i * kWarps, i);
@@ -428,7 +413,6 @@ rows_q8_kernel(const __grid_constant__ Q8Args args) {
       for (int i = 0; i < 4; ++i) st.o[mt][n][i] = 0.f;
   }
   // query rows: f16 with the row's own power of two
-  if constexpr (G::kQueriesInSmem) st.q_smem = reinterpret_cast<const uint2*>(base + G::kQueries0) + lane;
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
     uint32_t w[D / 8];
@@ -445,44 +429,33 @@ rows_q8_kernel(const __grid_constant__ Q8Args args) {
     const float f = exp2_int(-e);
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) {
-      const uint32_t lo = bf16x2_to_f16x2(w[2 * j], f), hi = bf16x2_to_f16x2(w[2 * j + 1], f);
-      if constexpr (G::kQueriesInSmem) {
-        if (warp == n) reinterpret_cast<uint2*>(base + G::kQueries0)[(n * (D / 16) + j) * 32 + lane] = make_uint2(lo, hi);
-      } else {
-        st.q[n][j][0] = lo;
-        st.q[n][j][1] = hi;
-      }
+      st.q[n][j][0] = bf16x2_to_f16x2(w[2 * j], f);
+      st.q[n][j][1] = bf16x2_to_f16x2(w[2 * j + 1], f);
     }
     const float mult = p.scale2 * exp2_int(e);
     st.mult[n][0] = __shfl_sync(0xffffffffu, mult, 8 * t);
     st.mult[n][1] = __shfl_sync(0xffffffffu, mult, 8 * t + 4);
   }
-  if constexpr (G::kQueriesInSmem) __syncthreads();
 
   // Tree nodes come first: their keys and values are fetched while the first copies are on their way.  (The warp's units are
   // first, first + kWarps, ..; those behind the prefix are the tree's.)
 #pragma unroll 1
   for (int unit = first + (max(p.TPH - first, 0) + kWarps - 1) / kWarps * kWarps; unit < end; unit += kWarps) {
-    // ancestors of node `lane` (T <= 32 here)
-    const int par = lane < p.T ? a.parent[lane] : -1;
-    uint32_t anc = 0u;
-    int u = lane < p.T ? lane : -1;
+    const int node0 = (unit - p.TPH) * kGroupKeys;
+    // which of the unit's 16 nodes the node of row `lane` sees: itself and its ancestors
+    uint32_t seen = 0u;
     bool bad = false;
+    int u = row0 + lane < p.rows ? (row0 + lane) >> log_g : -1;
 #pragma unroll 1
-    for (int i = 0; i < p.T; ++i) {
-      const int pu = __shfl_sync(0xffffffffu, par, u & 31);
-      if (u >= 0) {
-        anc |= 1u << u;
-        if (pu < -1 || pu >= u) {
-          bad = true;
-          u = -1;
-        } else {
-          u = pu;
-        }
-      }
+    for (int i = 0; i < p.T && u >= 0; ++i) {
+      if ((unsigned)(u - node0) < (unsigned)kGroupKeys) seen |= 1u << (u - node0);
+      const int pu = a.parent[u];
+      u = pu < u ? pu : -1;
     }
-    if (bad && head == 0) spx_raise(a.status, SPECEXT_ERR_BAD_TREE);
-    tree_step<D, NR>(st, a, head, (unit - p.TPH) * kGroupKeys, 0, log_g, anc, lane);
+    for (int v = lane; v < p.T; v += 32) bad |= a.parent[v] < -1 || a.parent[v] >= v;
+    if (bad) spx_raise(a.status, SPECEXT_ERR_BAD_TREE);
+    __syncwarp();
+    tree_step<D, NR>(st, a, head, node0, seen, lane);
   }
   int stage = 0;
 #pragma unroll 1
@@ -526,7 +499,7 @@ rows_q8_kernel(const __grid_constant__ Q8Args args) {
     }
   __syncthreads();
   if constexpr (!CLUSTER) {
-    const int slot = worker + head;
+    const int slot = worker + prob;                      // (one row block: the merge kernel's blocks have 32 rows)
     float* po = a.ws + p.off_part_o + (long long)slot * kCols * p.RB * 4;
     for (int i = tid; i < n_rows * kCols; i += kThreads) {
       const int col = i / n_rows, row = i - col * n_rows;
@@ -575,7 +548,7 @@ rows_q8_kernel(const __grid_constant__ Q8Args args) {
         acc.w = fmaf(f, x.w, acc.w);
       }
       const float inv = 1.f / Z;
-      const int node = row >> log_g, h = head * p.G + (row & (p.G - 1));
+      const int node = (row0 + row) >> log_g, h = head * p.G + ((row0 + row) & (p.G - 1));
       *reinterpret_cast<uint2*>(a.O + (long long)node * a.o_st + (long long)h * a.o_sh + col * 4) =
           make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
       if (col == 0) a.lse[(long long)h * p.T + node] = (M + log2f(Z)) * kLn2;
@@ -607,9 +580,7 @@ cudaError_t launch(const Q8Args& q, cudaStream_t st) {
 
 template <int D, bool CLUSTER>
 cudaError_t launch_rows(const Q8Args& q, cudaStream_t st) {
-  return q.a.plan.rows <= 8    ? launch<D, 1, CLUSTER>(q, st)
-         : q.a.plan.rows <= 16 ? launch<D, 2, CLUSTER>(q, st)
-                               : launch<D, 4, CLUSTER>(q, st);
+  return q.a.plan.q_rows == 8 ? launch<D, 1, CLUSTER>(q, st) : launch<D, 2, CLUSTER>(q, st);
 }
 
 }  // namespace
@@ -621,12 +592,12 @@ int spx_rows_q8_max_clusters(int dev, int size) {
   if (dev < 0 || dev >= kSpxMaxDevices || size < 1 || size > kMaxCluster) return 0;
   int n = known[dev][size].load();
   if (n > 0) return n - 1;
-  auto* kernel = rows_q8_kernel<128, 4, true>;
+  auto* kernel = rows_q8_kernel<128, 2, true>;
   static SpxOncePerDevice once;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(size);
-  cfg.blockDim = dim3(Geo<128, 4>::kThreads);
-  cfg.dynamicSmemBytes = Geo<128, 4>::kBytes;
+  cfg.blockDim = dim3(Geo<128, 2>::kThreads);
+  cfg.dynamicSmemBytes = Geo<128, 2>::kBytes;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = size;
@@ -634,7 +605,7 @@ int spx_rows_q8_max_clusters(int dev, int size) {
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (spx_opt_in_smem(kernel, Geo<128, 4>::kBytes, &once, true) != cudaSuccess ||
+  if (spx_opt_in_smem(kernel, Geo<128, 2>::kBytes, &once, true) != cudaSuccess ||
       cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
     (void)cudaGetLastError();
     return 0;
