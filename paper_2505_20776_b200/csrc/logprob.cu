@@ -5,13 +5,15 @@
 // cluster where rows are few, and joined in the first CTA's shared memory.
 //
 // The best words are found without sorting: a word's key is (logit, lower index first).  Every thread knows its own best key
-// after the pass; the lowest of the j-th best thread keys of the warps, with j times the number of warps >= k, bounds the k-th
-// best key of the CTA from below, so only threads with a key that good look at their words again (from L2), and the few words
-// above the bound are put in order by counting.  Words that are too many for the list (values arranged so that one thread has
-// them all) are taken out one by one.
+// after the pass; the k-th best of the warps' j best thread keys (j times the number of warps >= k) bounds the k-th best key of
+// the CTA from below, so only the vectors of threads with a key that good are looked at again (from L2, all of them
+// dealt to all threads: when each such thread looked through its own, with the rest of its warp waiting, that took longer than
+// the pass), and the few words above the bound are put in order by counting.  Words that are too many for the list (values
+// arranged so that one thread has them all) are taken out one by one.
 //
 // What bounds it: reading the logits (HBM), the exponentials (16 a cycle and SM) close behind for bf16; for few rows the chain of
 // latencies: load, reduction, second look, join.
+#include <cstdlib>
 #include "common.cuh"
 #include "pair.cuh"
 
@@ -21,7 +23,6 @@ using namespace pair;
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kVecs = 4;                        // 16-byte loads of a thread in flight
 constexpr int kMaxBest = 32, kMaxSlices = 8, kList = 512;
 constexpr float kLn2 = 0.693147180559945309417f, kLog2e = 1.44269504088896340736f;
 typedef unsigned long long Key;                 // 0: none
@@ -47,6 +48,7 @@ __device__ __forceinline__ Key make_key(float x, int idx) { return ((Key)ordered
 template <bool F32>
 struct Row {
   static constexpr int kWords = F32 ? 4 : 8;
+  static constexpr int kVecs = F32 ? 4 : 2;     // 16-byte loads of a thread at once, and as many for the next turn
   const char* base;                             // of the row, at most 15 bytes below its first word
   int skew, V, n_vec;
   __device__ __forceinline__ Row(const LogprobArgs& a, int row) {
@@ -63,60 +65,77 @@ struct Row {
   __device__ __forceinline__ int first_word(int v) const { return v * kWords - skew; }
 };
 
-// kVecs vectors v, v + kThreads, ... below `end` as floats; words outside are -inf.
+// Vector v of the row; words outside are -inf.
 template <bool F32>
-__device__ __forceinline__ void load_chunk(const Row<F32>& row, int v, int end, float (&x)[kVecs][Row<F32>::kWords]) {
+__device__ __forceinline__ uint4 load_vec(const Row<F32>& row, int v) {
   constexpr int W = Row<F32>::kWords;
-  uint4 r[kVecs];
-  bool whole[kVecs];
+  const int w0 = row.first_word(v);
+  if (w0 >= 0 && w0 <= row.V - W) return *reinterpret_cast<const uint4*>(row.base + (long long)v * 16);
+  uint32_t q[4];
 #pragma unroll
-  for (int i = 0; i < kVecs; ++i) {
-    const int u = v + i * kThreads, w0 = row.first_word(u);
-    whole[i] = u < end && w0 >= 0 && w0 <= row.V - W;
-    if (whole[i]) r[i] = *reinterpret_cast<const uint4*>(row.base + (long long)u * 16);
-  }
-#pragma unroll
-  for (int i = 0; i < kVecs; ++i) {
-    const int u = v + i * kThreads, w0 = row.first_word(u);
-    if (whole[i]) {
-      const uint32_t q[4] = {r[i].x, r[i].y, r[i].z, r[i].w};
-#pragma unroll
-      for (int j = 0; j < W; ++j)
-        x[i][j] = F32 ? __uint_as_float(q[j % 4]) : __uint_as_float(j & 1 ? q[j / 2 % 4] & 0xffff0000u : q[j / 2 % 4] << 16);
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (F32) {
+      q[i] = w0 + i >= 0 && w0 + i < row.V ? __float_as_uint(row.word(w0 + i)) : 0xff800000u;
     } else {
-#pragma unroll
-      for (int j = 0; j < W; ++j) x[i][j] = u < end && w0 + j >= 0 && w0 + j < row.V ? row.word(w0 + j) : -INFINITY;
+      const int w = w0 + 2 * i;
+      q[i] = (w >= 0 && w < row.V ? __float_as_uint(row.word(w)) >> 16 : 0xff80u) |
+             (w + 1 >= 0 && w + 1 < row.V ? __float_as_uint(row.word(w + 1)) & 0xffff0000u : 0xff800000u);
     }
   }
+  return make_uint4(q[0], q[1], q[2], q[3]);
+}
+template <bool F32>
+__device__ __forceinline__ void unpack(uint4 r, float (&x)[Row<F32>::kWords]) {
+  const uint32_t q[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int j = 0; j < Row<F32>::kWords; ++j)
+    x[j] = F32 ? __uint_as_float(q[j % 4]) : __uint_as_float(j & 1 ? q[j / 2 % 4] & 0xffff0000u : q[j / 2 % 4] << 16);
 }
 
+// Statistics of some words: m their largest logit; with t(x) = x c - m c (c: log2 e / temperature), z the sum of 2^t, e that of
+// 2^t t.  m c is rounded once, and every use rounds it alike, so that it takes no part in the error.  Where even m is a mask (a row
+// of nothing but the type's lowest value), m c might overflow and t is (x - m) c.
 struct Stat {
-  float m, z, e;                                // of raw logits: e is the sum of e^((raw - m) / temperature) (raw - m)
+  float m, z, e;
 };
-__device__ __forceinline__ Stat join(Stat a, Stat b, float c) {
-  const float m = fmaxf(a.m, b.m);
-  Stat r = {m, 0.f, 0.f};
-  if (a.z != 0.f) {                             // (also a NaN)
-    const float d = a.m - m, f = ex2_approx(d * c);
-    r.z = a.z * f;
-    r.e = f == 0.f ? 0.f : f * fmaf(d, a.z, a.e);
-  }
-  if (b.z != 0.f) {
-    const float d = b.m - m, f = ex2_approx(d * c);
-    r.z = fmaf(b.z, f, r.z);
-    r.e += f == 0.f ? 0.f : f * fmaf(d, b.z, b.e);
-  }
-  return r;
+constexpr float kMask = -1e36f;
+// `s` relative to a maximum m >= s.m.
+__device__ __forceinline__ Stat at_maximum(Stat s, float m, float c) {
+  const float d = m > kMask ? __fsub_rn(__fmul_rn(s.m, c), __fmul_rn(m, c)) : (s.m - m) * c, f = ex2_approx(d);
+  // (z = 0: no word, or none but -inf; f = 0: nothing is left of it, whatever d is)
+  if (s.z == 0.f) return {m, 0.f, 0.f};
+  return {m, s.z * f, f == 0.f ? 0.f : f * fmaf(d, s.z, s.e)};
 }
+// The joint statistics of stats[0 .. n), n <= 8, by every warp for itself: a lane has one of them.
+__device__ __forceinline__ Stat join(const Stat* stats, int n, float c) {
+  const int i = threadIdx.x & 7;
+  Stat s = {-INFINITY, 0.f, 0.f};
+  if (i < n) s = stats[i];
+  float m = s.m;
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  s = at_maximum(s, m, c);
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) {
+    s.z += __shfl_xor_sync(0xffffffffu, s.z, o);
+    s.e += __shfl_xor_sync(0xffffffffu, s.e, o);
+  }
+  return s;
+}
+static_assert(kWarps <= 8 && kMaxSlices <= 8, "join has 8 lanes");
 
 struct Shared {
   Stat warp_stat[kWarps];
-  Key warp_bound[kWarps];
+  Key bounds[kWarps * kMaxBest];                // the warps' best thread keys
   Key list[kList];
   Key top[kMaxBest];
-  int n_list;
-  Stat stat[kMaxSlices];                        // in the first CTA, from all of the cluster
-  Key keys[kMaxSlices][kMaxBest];
+  int n_list, n_again;
+  unsigned char again[kThreads];                // threads whose vectors are looked at again
+  // in the first CTA of a cluster, from all of it
+  Stat stat[kMaxSlices];
+  Key keys[kMaxSlices * kMaxBest];
+  uint64_t arrived;
+  int abort_flag;
 };
 
 __device__ __forceinline__ Key warp_max_key(Key k) {
@@ -131,66 +150,59 @@ __device__ __forceinline__ void in_order(const Key* keys, int n, Put&& put) {
   for (int i = threadIdx.x; i < n; i += kThreads) {
     const Key mine = keys[i];
     int place = 0;
+#pragma unroll 4
     for (int j = 0; j < n; ++j) place += keys[j] > mine ? 1 : 0;
     if (mine != 0) put(place, mine);
   }
 }
 
-// The `best` best keys of the words in vectors [lo, hi) to sh.top, in order (zeros where there are no more words).
-template <bool F32>
-__device__ __forceinline__ void best_words(Shared& sh, const Row<F32>& row, int lo, int hi, int best, float top_value, int top_v) {
+// use(key) for every word of vector v (NaN has none).
+template <bool F32, class Use>
+__device__ __forceinline__ void each_key(const Row<F32>& row, int v, Use&& use) {
   constexpr int W = Row<F32>::kWords;
+  float x[W];
+  unpack<F32>(load_vec(row, v), x);
+#pragma unroll
+  for (int j = 0; j < W; ++j) {
+    const int idx = row.first_word(v) + j;
+    if (x[j] == x[j] && idx >= 0 && idx < row.V) use(make_key(x[j], idx));
+  }
+}
+
+// The `best` best keys of the words in vectors [lo, hi) to sh.top, in order (zeros where there are no more words), from the
+// threads' best keys; `full` warps had a vector for every thread, and their best thread keys are in sh.bounds.
+template <bool F32>
+__device__ __forceinline__ void best_words(Shared& sh, const Row<F32>& row, int lo, int hi, int best, Key mine, int full) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  Key mine = 0;
-  if (top_v >= 0) {
-    float x[kVecs][W];
-    load_chunk(row, top_v, hi, x);
-#pragma unroll
-    for (int i = kVecs - 1; i >= 0; --i)
-#pragma unroll
-      for (int j = W - 1; j >= 0; --j) {
-        const int idx = row.first_word(top_v + i * kThreads) + j;
-        if (x[i][j] == top_value && top_v + i * kThreads < hi && idx >= 0 && idx < row.V) mine = make_key(x[i][j], idx);
-      }
-  }
-  // the bound: whole warps of threads with a key, j-th best of each
-  const int full = min(kWarps, (hi - lo) / 32);
+  // The bound: of the warps' best thread keys (j of each, at least k in all) the k-th best; or the lowest, where they are too many
+  // for a warp to look at.
+  const int j = full > 0 ? (best + full - 1) / full : 0, n_bounds = j * full;
   Key bound = 0;
-  if (full > 0 && warp < full) {
-    const int j = (best + full - 1) / full;
-    if (j <= 32) {
-      Key k = mine;
-      for (int i = 0; i < j; ++i) {
-        bound = warp_max_key(k);
-        if (k == bound) k = 0;
-      }
-    }
+  if (n_bounds > 0 && n_bounds <= 32) {
+    const Key k = lane < n_bounds ? sh.bounds[lane] : 0;
+    int place = 0;
+#pragma unroll 4
+    for (int i = 0; i < n_bounds; ++i) place += sh.bounds[i] > k ? 1 : 0;
+    // (a zero key: a thread that has none but NaN; then the bound is none)
+    const unsigned who = __ballot_sync(0xffffffffu, lane < n_bounds && place == best - 1);
+    bound = who ? __shfl_sync(0xffffffffu, k, __ffs(who) - 1) : 0;
+  } else if (n_bounds > 0) {
+    bound = sh.bounds[j - 1];
+    for (int i = 1; i < full; ++i) bound = min(bound, sh.bounds[i * j + j - 1]);
   }
-  if (lane == 0) sh.warp_bound[warp] = bound;
-  if (tid < kMaxBest) sh.top[tid] = 0;
-  if (tid == 0) sh.n_list = 0;
+  if (mine != 0 && mine >= bound) sh.again[atomicAdd(&sh.n_again, 1)] = (unsigned char)tid;
   __syncthreads();
-  bound = full > 0 ? sh.warp_bound[0] : 0;
-  for (int i = 1; i < full; ++i) bound = min(bound, sh.warp_bound[i]);
-  if (mine >= bound && mine != 0) {
-    for (int v = lo + tid; v < hi; v += kVecs * kThreads) {
-      float x[kVecs][W];
-      load_chunk(row, v, hi, x);
-#pragma unroll
-      for (int i = 0; i < kVecs; ++i)
-#pragma unroll
-        for (int j = 0; j < W; ++j) {
-          const int u = v + i * kThreads, idx = row.first_word(u) + j;
-          if (x[i][j] == x[i][j] && u < hi && idx >= 0 && idx < row.V) {
-            const Key k = make_key(x[i][j], idx);
-            if (k >= bound) {
-              const int at = atomicAdd(&sh.n_list, 1);
-              if (at < kList) sh.list[at] = k;
-            }
-          }
+  const int per = (hi - lo + kThreads - 1) / kThreads, n_again = sh.n_again;
+  // 8 to 32 threads to each of those threads' vectors
+  const int log_team = per > 16 ? 5 : per > 8 ? 4 : 3, member = tid & ((1 << log_team) - 1);
+  for (int q = tid >> log_team; q < n_again; q += kThreads >> log_team)
+    for (int v = lo + sh.again[q] + member * kThreads; v < hi; v += kThreads << log_team)
+      each_key(row, v, [&](Key k) {
+        if (k >= bound) {
+          const int at = atomicAdd(&sh.n_list, 1);
+          if (at < kList) sh.list[at] = k;
         }
-    }
-  }
+      });
   __syncthreads();
   const int n = sh.n_list;
   if (n <= kList) {
@@ -199,22 +211,13 @@ __device__ __forceinline__ void best_words(Shared& sh, const Row<F32>& row, int 
     });
   } else {
     Key before = ~0ull;
+#pragma unroll 1
     for (int r = 0; r < best; ++r) {
       Key k = 0;
-      for (int v = lo + tid; v < hi; v += kVecs * kThreads) {
-        float x[kVecs][W];
-        load_chunk(row, v, hi, x);
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i)
-#pragma unroll
-          for (int j = 0; j < W; ++j) {
-            const int u = v + i * kThreads, idx = row.first_word(u) + j;
-            if (x[i][j] == x[i][j] && u < hi && idx >= 0 && idx < row.V) {
-              const Key q = make_key(x[i][j], idx);
-              if (q < before && q > k) k = q;
-            }
-          }
-      }
+      for (int v = lo + tid; v < hi; v += kThreads)
+        each_key(row, v, [&](Key q) {
+          if (q < before && q > k) k = q;
+        });
       k = warp_max_key(k);
       __syncthreads();                          // (the round before has been read)
       if (lane == 0) sh.list[warp] = k;
@@ -228,106 +231,199 @@ __device__ __forceinline__ void best_words(Shared& sh, const Row<F32>& row, int 
 }
 
 template <bool F32>
-__global__ void __launch_bounds__(kThreads) logprob_kernel(const __grid_constant__ LogprobArgs a) {
-  constexpr int W = Row<F32>::kWords;
+__global__ void __launch_bounds__(kThreads, 4) logprob_kernel(const __grid_constant__ LogprobArgs a) {
+  constexpr int W = Row<F32>::kWords, kVecs = Row<F32>::kVecs;
   __shared__ Shared sh;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int n_slices = a.slices, r = (int)blockIdx.x / n_slices, rank = (int)blockIdx.x - r * n_slices;
-  if (n_slices > 1) cluster_arrive_relaxed();   // (waited for before the first write to another CTA)
+  if (tid < kMaxBest) sh.top[tid] = 0;
+  if (tid == 0) {
+    sh.n_list = sh.n_again = 0;
+    if (n_slices > 1) {
+      sh.abort_flag = 0;
+      mbar_init(&sh.arrived, 1);
+      fence_mbar_init();
+      if (rank == 0) mbar_arrive_expect_tx(&sh.arrived, n_slices * (a.best * 8 + 12));
+    }
+  }
+  if (n_slices > 1) {
+    __syncwarp();
+    cluster_arrive();                           // (waited for before the first write to another CTA)
+  }
   pdl_launch_dependents();
   const Row<F32> row(a, r);
   const int per = (row.n_vec + n_slices - 1) / n_slices;
   const int lo = min(row.n_vec, rank * per), hi = min(row.n_vec, lo + per);
   const float c = a.inv_temperature * kLog2e;
   pdl_wait();
+  // the first given tokens' logits, ahead of the pass
+  int token = -1;
+  float given = -INFINITY;
+  if (rank == 0 && tid < a.given) {
+    token = a.tokens[(long long)r * a.given + tid];
+    if (token >= 0 && token < a.V) given = row.word(token);
+  }
 
   Stat s = {-INFINITY, 0.f, 0.f};
   float top_value = -INFINITY;
   int top_v = -1;
-  for (int v = lo + tid; v < hi; v += kVecs * kThreads) {
-    float x[kVecs][W];
-    load_chunk(row, v, hi, x);
-    float m = -INFINITY;
+  uint4 top_raw = make_uint4(0u, 0u, 0u, 0u);
+  uint4 next[kVecs];
+  auto fetch = [&](int v) {
 #pragma unroll
     for (int i = 0; i < kVecs; ++i)
+      next[i] = v + i * kThreads < hi ? load_vec(row, v + i * kThreads)
+                                      : (F32 ? make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u)
+                                             : make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u));
+  };
+  fetch(lo + tid);
+  const uint64_t c2 = pack_f32x2(c, c);
+  for (int v = lo + tid; v < hi; v += kVecs * kThreads) {
+    uint4 raw[kVecs];
+    float x[kVecs][W], vm[kVecs], m = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < W; j += 2) m = fmax3(m, x[i][j], x[i][j + 1]);
+    for (int i = 0; i < kVecs; ++i) raw[i] = next[i];
+    if (v + kVecs * kThreads < hi) fetch(v + kVecs * kThreads);
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      unpack<F32>(raw[i], x[i]);
+      vm[i] = fmaxf(x[i][0], x[i][1]);
+#pragma unroll
+      for (int j = 2; j < W; j += 2) vm[i] = fmax3(vm[i], x[i][j], x[i][j + 1]);
+      m = fmaxf(m, vm[i]);
+    }
     if (m > top_value || top_v < 0) {
       top_value = m;
       top_v = v;
-    }
-    if (m > s.m) {
-      if (s.z != 0.f) {                         // (s.m is finite then)
-        const float d = s.m - m, f = ex2_approx(d * c);
-        s.e = f == 0.f ? 0.f : f * fmaf(d, s.z, s.e);
-        s.z *= f;
-      }
-      s.m = m;
-    }
-    const float m0 = s.m == -INFINITY ? 0.f : s.m;
-    float z = 0.f, e = 0.f;
+      top_raw = raw[0];
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i)
+      for (int i = kVecs - 1; i > 0; --i)       // (the first vector that has the maximum, and that exists)
+        if (vm[i] == m && vm[0] != m) {
+          top_v = v + i * kThreads;
+          top_raw = raw[i];
+        }
+    }
+    if (m > s.m) s = at_maximum(s, m, c);
+    if (s.m > kMask) {
+      const float neg = -__fmul_rn(s.m, c);
+      const uint64_t neg2 = pack_f32x2(neg, neg);
+      uint64_t z = 0ull, e = 0ull;
 #pragma unroll
-      for (int j = 0; j < W; ++j) {
-        const float d = x[i][j] - m0, q = ex2_approx(d * c);
-        z += q;
-        e = fmaf(q, fmaxf(d, -1e30f), e);       // (a word masked out: 0 times a large number, not times infinity)
+      for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+        for (int j = 0; j < W; j += 2) {
+          float t0, t1;
+          unpack_f32x2(fma_f32x2(pack_f32x2(x[i][j], x[i][j + 1]), c2, neg2), t0, t1);
+          const uint64_t q = pack_f32x2(ex2_approx(t0), ex2_approx(t1));
+          z = add_f32x2(z, q);
+          // (a word masked out: 0 times a large number, not times infinity)
+          e = fma_f32x2(q, pack_f32x2(fmaxf(t0, -1e30f), fmaxf(t1, -1e30f)), e);
+        }
+      float z0, z1, e0, e1;
+      unpack_f32x2(z, z0, z1);
+      unpack_f32x2(e, e0, e1);
+      s.z += z0 + z1;
+      s.e += e0 + e1;
+    } else {
+      // nothing but masks and NaN so far: word by word
+      const float m0 = s.m == -INFINITY ? 0.f : s.m;
+#pragma unroll 1
+      for (int i = 0; i < kVecs * W; ++i) {
+        const int u = v + i / W * kThreads, idx = row.first_word(u) + i % W;
+        if (u >= hi || idx < 0 || idx >= row.V) continue;
+        const float t = (row.word(idx) - m0) * c, q = ex2_approx(t);
+        s.z += q;
+        s.e = fmaf(q, fmaxf(t, -1e30f), s.e);
       }
-    s.z += z;
-    s.e += e;
+    }
   }
-  if (a.best > 0) best_words(sh, row, lo, hi, a.best, top_value, top_v);
 
+  // warp: statistics, and the j-th best of its threads' best keys
+  float m = s.m;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  s = at_maximum(s, m, c);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    const Stat b = {__shfl_xor_sync(0xffffffffu, s.m, o), __shfl_xor_sync(0xffffffffu, s.z, o), __shfl_xor_sync(0xffffffffu, s.e, o)};
-    s = join(s, b, c);
+    s.z += __shfl_xor_sync(0xffffffffu, s.z, o);
+    s.e += __shfl_xor_sync(0xffffffffu, s.e, o);
   }
   if (lane == 0) sh.warp_stat[warp] = s;
-  __syncthreads();
-  s = sh.warp_stat[0];
+  const int full = min(kWarps, (hi - lo) / 32);           // warps with a vector for every thread
+  Key mine = 0;
+  if (a.best > 0) {
+    if (top_v >= 0) {
+      float x[W];
+      unpack<F32>(top_raw, x);
 #pragma unroll
-  for (int i = 1; i < kWarps; ++i) s = join(s, sh.warp_stat[i], c);
+      for (int j = W - 1; j >= 0; --j) {
+        const int idx = row.first_word(top_v) + j;
+        if (x[j] == top_value && idx >= 0 && idx < row.V) mine = make_key(x[j], idx);
+      }
+    }
+    if (warp < full) {
+      Key k = mine;
+      const int j = (a.best + full - 1) / full;
+#pragma unroll 1
+      for (int i = 0; i < j; ++i) {
+        const Key top = warp_max_key(k);
+        if (lane == 0) sh.bounds[warp * j + i] = top;
+        if (k == top) k = 0;
+      }
+    }
+  }
+  __syncthreads();
+  s = join(sh.warp_stat, kWarps, c);
+  if (a.best > 0) best_words(sh, row, lo, hi, a.best, mine, full);
 
   const Key* keys = sh.top;
   int n_keys = a.best;
   if (n_slices > 1) {
     cluster_wait();                             // every CTA of the cluster has started
+    const uint32_t bar = map_to_cta(smem_u32(&sh.arrived), 0);
     if (tid < a.best) {
-      const uint32_t at = map_to_cta(smem_u32(&sh.keys[0][0] + rank * a.best + tid), 0);
-      asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(at), "l"(sh.top[tid]) : "memory");
+      const uint32_t at = map_to_cta(smem_u32(&sh.keys[rank * a.best + tid]), 0);
+      asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(at), "l"(sh.top[tid]), "r"(bar)
+                   : "memory");
     }
-    if (tid == 0) {
-      const uint32_t at = map_to_cta(smem_u32(&sh.stat[rank]), 0);
-      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(s.m) : "memory");
-      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 4), "f"(s.z) : "memory");
-      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 8), "f"(s.e) : "memory");
+    if (tid >= kThreads - 3) {
+      const int i = tid - (kThreads - 3);
+      const uint32_t at = map_to_cta(smem_u32(&sh.stat[rank]) + 4 * i, 0);
+      asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(at),
+                   "r"(__float_as_uint(i == 0 ? s.m : i == 1 ? s.z : s.e)), "r"(bar)
+                   : "memory");
     }
-    cluster_sync();
     if (rank != 0) return;
-    s = sh.stat[0];
-    for (int i = 1; i < n_slices; ++i) s = join(s, sh.stat[i], c);
-    keys = &sh.keys[0][0];
+    if (!mbar_wait(&sh.arrived, 0, &sh.abort_flag)) {
+      if (lane == 0) spx_raise(a.status, SPECEXT_ERR_TIMEOUT);
+      settle();
+      return;
+    }
+    s = join(sh.stat, n_slices, c);
+    keys = sh.keys;
     n_keys = n_slices * a.best;
   }
 
   // log(z) of a row without a finite logit is -inf: all its log probabilities are, and its entropy is 0
   const bool empty = s.z == 0.f;
-  const float log_z = log2f(s.z) * kLn2, lse = empty ? -INFINITY : fmaf(s.m, a.inv_temperature, log_z);
+  // log Z relative to m itself: what m c was rounded by is put right
+  const float log2_z = log2f(s.z), off = s.m > kMask ? fmaf(s.m, c, -__fmul_rn(s.m, c)) : 0.f;
+  const float log_z = (log2_z - off) * kLn2, lse = empty ? -INFINITY : fmaf(s.m, a.inv_temperature, log_z);
   // (the difference to the maximum first: x - lse would lose log Z where the maximum is huge, as in a row of the type's lowest value)
   auto log_p = [&](float raw) { return empty ? -INFINITY : fmaf(raw - s.m, a.inv_temperature, -log_z); };
   if (tid == 0) {
     a.lse[r] = lse;
-    a.entropy[r] = empty ? 0.f : log_z - s.e * a.inv_temperature / s.z;
+    a.entropy[r] = empty ? 0.f : (log2_z - s.e / s.z) * kLn2;
   }
   for (int i = tid; i < a.given; i += kThreads) {
     const long long at = (long long)r * a.given + i;
-    const int t = a.tokens[at];
-    float lp = -INFINITY;                       // -1: no token
-    if (t >= 0 && t < a.V) lp = log_p(row.word(t));
-    else if (t != -1) spx_raise(a.status, SPECEXT_ERR_INVALID_ARG);
-    a.logprob[at] = lp;
+    if (i >= kThreads) {
+      token = a.tokens[at];
+      given = token >= 0 && token < a.V ? row.word(token) : -INFINITY;
+    }
+    const bool known = token >= 0 && token < a.V;
+    a.logprob[at] = known ? log_p(given) : -INFINITY;                          // -1: no token
+    if (!known && token != -1) spx_raise(a.status, SPECEXT_ERR_INVALID_ARG);
   }
   const bool bad = !(s.z == s.z);               // a NaN or +inf among the logits: no order
   in_order(keys, n_keys, [&](int place, Key k) {
@@ -371,10 +467,13 @@ cudaError_t spx_launch_logprobs(const void* logits, bool f32, int rows, int V, l
   a.logits = logits; a.tokens = tokens;
   a.logprob = logprob; a.entropy = entropy; a.lse = lse; a.top_ids = top_ids; a.top_logprob = top_logprob; a.status = status;
   a.stride = stride; a.V = V; a.given = given; a.best = best; a.inv_temperature = inv_temperature;
-  // CTAs per row: as many as fill the chip three times, as long as a thread still has a load of its own in every slice
+  // CTAs per row: as many as are resident at once (four per SM), as long as a thread has two vectors and more.  us per call, 1 / 2 /
+  // 4 / 8: one row of 32000 bf16 7.9 / 6.3 / 5.6 / 5.7, 16 of 128256 34 / 20 / 13 / 10, 60 of 128256 38 / 24 / 19 / 15, 200 of 32000
+  // fp32 17.0 / 13.8 / 16.8 / 23.0, 2047 of 32000 69 / 87 / 122 / 191
   const int words = f32 ? 4 : 8;
   int slices = 1;
-  while (slices < kMaxSlices && (long long)rows * slices < 3ll * n_sm && V / words >= 2 * slices * 2 * kThreads) slices *= 2;
+  while (slices < kMaxSlices && 2ll * rows * slices <= 4ll * n_sm && V / words >= 2 * slices * 2 * kThreads) slices *= 2;
+  if (getenv("SPX_SL")) slices = atoi(getenv("SPX_SL"));
   a.slices = slices;
   return f32 ? launch<true>(a, rows, st) : launch<false>(a, rows, st);
 }
