@@ -22,7 +22,7 @@ struct QuantArgs {
   int start, n, n_src, n_heads, log_block;
 };
 
-constexpr int kPerThread = 8;                   // 16-byte pieces of bf16 a thread holds
+constexpr int kPerThread = 4;                   // pieces of 16 values a thread holds
 constexpr uint32_t kScaleFloor = 27;            // 2^-100: of a block of zeros
 
 // The scale of a block whose largest magnitude has these bits.
@@ -40,11 +40,16 @@ __device__ __forceinline__ uint32_t scaled_e4m3x4(uint32_t codes, float f) {
   const float2 x = f16x2_to_f32x2(e4m3x2_to_f16x2(codes)), y = f16x2_to_f32x2(e4m3x2_to_f16x2(codes >> 16));
   return f32x2_to_e4m3x2(x.x * f, x.y * f) | (f32x2_to_e4m3x2(y.x * f, y.y * f) << 16);
 }
+// The larger magnitudes, half by half: bf16 without its sign orders as an integer does, infinities and NaN above all.
+__device__ __forceinline__ uint32_t magnitudes(uint32_t m, uint4 x) {
+  m = __vmaxu2(__vmaxu2(m, x.x & 0x7fff7fffu), x.y & 0x7fff7fffu);
+  return __vmaxu2(__vmaxu2(m, x.z & 0x7fff7fffu), x.w & 0x7fff7fffu);
+}
 
 // grid: (heads of every block touched, the head varying fastest; K and V); block: B * D / 64 threads.
 template <int D>
 __global__ void __launch_bounds__(256) quantize_kernel(const __grid_constant__ QuantArgs q) {
-  constexpr int kCols = D / 8;
+  constexpr int kCols = D / 16;
   __shared__ uint32_t warp_max[8];
   pdl_launch_dependents();
   const int nth = (int)blockIdx.x / q.n_heads, h = (int)blockIdx.x - nth * q.n_heads;
@@ -56,29 +61,28 @@ __global__ void __launch_bounds__(256) quantize_kernel(const __grid_constant__ Q
   const int lead = max(q.start - token0, 0), end = min(B, q.start + q.n - token0);      // new tokens: [lead, end) of the block
   pdl_wait();
   const uint32_t old = lead > 0 ? *scale : 0u;
-  uint4 v[kPerThread];
-  uint32_t m = 0u;
+  uint4 v[kPerThread][2];
   bool outside = false;
 #pragma unroll
   for (int k = 0; k < kPerThread; ++k) {
     const int i = threadIdx.x + k * blockDim.x, t = i / kCols, c = i % kCols;
-    v[k] = make_uint4(0u, 0u, 0u, 0u);
+    v[k][0] = v[k][1] = make_uint4(0u, 0u, 0u, 0u);
     if (t >= lead && t < end) {
       int row = token0 + t - q.start;
       if (q.rows) row = q.rows[row];
-      if (row >= 0 && row < q.n_src)
-        v[k] = *reinterpret_cast<const uint4*>(x + (long long)row * q.x_sl + (long long)h * q.x_sh + c * 8);
-      else
+      if (row >= 0 && row < q.n_src) {
+        const uint4* src = reinterpret_cast<const uint4*>(x + (long long)row * q.x_sl + (long long)h * q.x_sh + c * 16);
+        v[k][0] = src[0];
+        v[k][1] = src[1];
+      } else {
         outside = true;
+      }
     }
   }
+  uint32_t m2 = 0u;
 #pragma unroll
-  for (int k = 0; k < kPerThread; ++k) {
-    const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) m = max(m, max((w[j] << 16) & 0x7fffffffu, w[j] & 0x7fff0000u));
-  }
-  m = __reduce_max_sync(0xffffffffu, m);
+  for (int k = 0; k < kPerThread; ++k) m2 = magnitudes(magnitudes(m2, v[k][0]), v[k][1]);
+  uint32_t m = __reduce_max_sync(0xffffffffu, max(m2 << 16, m2 & 0xffff0000u));
   if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = m;
   __syncthreads();
   for (int i = 0; i < (int)blockDim.x >> 5; ++i) m = max(m, warp_max[i]);
@@ -94,12 +98,13 @@ __global__ void __launch_bounds__(256) quantize_kernel(const __grid_constant__ Q
 #pragma unroll
   for (int k = 0; k < kPerThread; ++k) {
     const int i = threadIdx.x + k * blockDim.x, t = i / kCols, c = i % kCols;
-    uint2* dst = reinterpret_cast<uint2*>(codes + (long long)(token0 + t) * q.c_sl + c * 8);
+    uint4* dst = reinterpret_cast<uint4*>(codes + (long long)(token0 + t) * q.c_sl + c * 16);
     if (t >= lead && t < end) {
-      *dst = make_uint2(bf16x4_to_e4m3x4(v[k].x, v[k].y, f), bf16x4_to_e4m3x4(v[k].z, v[k].w, f));
+      *dst = make_uint4(bf16x4_to_e4m3x4(v[k][0].x, v[k][0].y, f), bf16x4_to_e4m3x4(v[k][0].z, v[k][0].w, f),
+                        bf16x4_to_e4m3x4(v[k][1].x, v[k][1].y, f), bf16x4_to_e4m3x4(v[k][1].z, v[k][1].w, f));
     } else if (t < lead && grown) {
-      const uint2 o = *dst;
-      *dst = make_uint2(scaled_e4m3x4(o.x, ratio), scaled_e4m3x4(o.y, ratio));
+      const uint4 o = *dst;
+      *dst = make_uint4(scaled_e4m3x4(o.x, ratio), scaled_e4m3x4(o.y, ratio), scaled_e4m3x4(o.z, ratio), scaled_e4m3x4(o.w, ratio));
     }
   }
 }
@@ -120,7 +125,7 @@ cudaError_t spx_launch_quantize(const void* K, const void* V, int n_kv_heads, in
   const int first = start >> log_block, last = (start + n - 1) >> log_block;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)n_kv_heads * (unsigned)(last - first + 1), 2);
-  cfg.blockDim = dim3((head_dim << log_block) / (8 * kPerThread));
+  cfg.blockDim = dim3((head_dim << log_block) / (16 * kPerThread));
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
