@@ -144,11 +144,12 @@ int specext_quantize_kv(const void* K, const void* V, int32_t n_src, int32_t n_k
  * are those of K_codes and V_codes, in bytes and multiples of 16; the tree's keys and values are bf16.  Codes and scales
  * at and behind prefix_len are never used; the codes 0x7F and 0xFF (NaN), which specext_quantize_kv does not write
  * to a block with a finite scale, are NaN.
- * Arithmetic: the result is that of attention on the values the cache stands for.  Codes are multiplied
- * as f16 (exact), queries and tree keys and values as f16 with a power of two per row or 32 nodes (exact but for values
- * 2^-28 and more below the largest); products are accumulated in fp32; probabilities, times the V scale, are rounded to f16 for
- * the product with V (11 bits; 2^-30 and less of a row's largest counts as zero); chunk sums and the normaliser are accumulated in
- * fp32 from unrounded exponentials.  Everything else as in specext_verify_attn, chunk_score included, so that
+ * Arithmetic: the result is that of attention on the values the cache stands for (magnitudes up to 2^100).  Products
+ * of queries and codes are exact but for query and tree values that lie far below the largest of their row or of
+ * their 32 nodes (those 2^-10 of it and less are kept to 2^-18 of it, for up to 16 rows per KV head to 2^-39) and are
+ * accumulated in fp32; probabilities, times the V scale, are rounded to f16 for the product with V (11 bits;
+ * 2^-30 and less of a row's largest counts as zero); chunk sums and the normaliser are accumulated in fp32 from
+ * unrounded exponentials.  Everything else as in specext_verify_attn, chunk_score included, so that
  * SelectChunks and UpdateDraftCache follow unchanged.  The workspace has a size of its own.
  */
 size_t specext_verify_attn_q8_workspace(const specext_attn_desc* desc, const specext_q8_desc* q8);

@@ -147,15 +147,14 @@ __device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, volati
   return __all_sync(0xffffffffu, wait_c(bar, parity, abort_flag));
 }
 
-// A warp's arrival on a barrier of the leader, behind its plain stores to shared memory that the pair's MMAs read.
+// A warp's arrival on a barrier of the leader, behind its plain stores of MMA operands to this CTA's shared memory.  They are read
+// by the tensor cores of this SM alone, and the proxy fence has them in place for those; what the arrival tells the leader, which
+// may be the other CTA, is only that.  (Releasing at the cluster's scope takes 1100 to 1900 cycles, longer than a tile.)
 template <int PAIR>
 __device__ __forceinline__ void publish(uint64_t* bar, int lane) {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   __syncwarp();
-  if (lane == 0) {
-    if constexpr (PAIR == 2) arrive_release_cluster(map_to_cta(smem_u32(bar), 0));
-    else mbar_arrive(bar);
-  }
+  if (lane == 0) arrive_cluster(leader_addr<PAIR>(bar));
 }
 
 // Place of 16-byte column `col` of row `row` in a block of f16 (or bf16): blocks of 64 elements, 128-byte swizzle.
@@ -193,8 +192,11 @@ __device__ __forceinline__ uint32_t amax_bf16x8(uint32_t m, uint4 x) {
   return amax_bf16x2(amax_bf16x2(amax_bf16x2(amax_bf16x2(m, x.x), x.y), x.z), x.w);
 }
 // High and low parts of four bf16 values times f.  As f16 the values are exact (8 bits, at most 2^8), and so is the difference.
+// An infinity becomes NaN, which e4m3 has (the conversion would make it 448).
 __device__ __forceinline__ void split4(uint32_t a, uint32_t b, float f, uint32_t& hi, uint32_t& lo) {
-  const uint32_t x0 = bf16x2_to_f16x2(a, f), x1 = bf16x2_to_f16x2(b, f);
+  uint32_t x0 = bf16x2_to_f16x2(a, f), x1 = bf16x2_to_f16x2(b, f);
+  x0 = add_f16x2(x0, sub_f16x2(x0, x0));
+  x1 = add_f16x2(x1, sub_f16x2(x1, x1));
   const uint32_t h0 = f16x2_to_e4m3x2(x0), h1 = f16x2_to_e4m3x2(x1);
   hi = h0 | (h1 << 16);
   lo = f16x2_to_e4m3x2(sub_f16x2(x0, e4m3x2_to_f16x2(h0))) | (f16x2_to_e4m3x2(sub_f16x2(x1, e4m3x2_to_f16x2(h1))) << 16);
@@ -473,15 +475,8 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
       ok = mbar_wait(&ctl8->vc_full[vc], vcph, abort_flag) && wait_c(&ctl->v_empty[vst], vph, abort_flag);
       if (!ok) break;
       expand_key<G::kVRow>(base + G::v8_off + vc * G::kVUnit, base + G::v_off + vst * G::kVStage, key);
-      // The stores are read by the tensor cores of this SM alone, and the proxy fence has them in place for those; what the arrival
-      // tells the leader, which may be the other CTA, is only that.  (Releasing at the cluster's scope takes 1100 to 1900 cycles,
-      // longer than a tile.)
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) {
-        arrive_cluster(leader_addr<PAIR>(&ctl->v_full[vst]));
-        mbar_arrive(&ctl8->vc_empty[vc]);
-      }
+      publish<PAIR>(&ctl->v_full[vst], lane);
+      if (lane == 0) mbar_arrive(&ctl8->vc_empty[vc]);
       if (++vc == G::kVUnits) {
         vc = 0;
         vcph ^= 1;
@@ -534,8 +529,7 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
       if (ok && key == 0) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          if constexpr (PAIR == 2) arrive_release_cluster(map_to_cta(smem_u32(&ctl8->k_full[u[i]]), 0));
-          else mbar_arrive(&ctl8->k_full[u[i]]);
+          arrive_cluster(leader_addr<PAIR>(&ctl8->k_full[u[i]]));
         }
       }
       if (ok) ok = wait_c(&ctl->v_empty[vst], vph, abort_flag);
