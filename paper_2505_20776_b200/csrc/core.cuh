@@ -205,11 +205,13 @@ __device__ __forceinline__ void finish(Ctrl* ctl, int warp) {
 // Two threads of the leader CTA issue the S and the PV MMAs.  (A thread that issues an MMA is held until the tensor pipe
 // takes it, and its waits, commits and bookkeeping cost it another ~0.5 K cycles a tile: one thread for both kinds left
 // the pipe idle that long, 2.1 K cycles a tile against 1.0 K of MMAs.)  `Work` enumerates the segments (`next()`, `n`
-// tiles in the current one).  F16: the operands are f16 instead of bf16.
-template <int PAIR, int D, bool F16 = false, class G, class Work>
-__device__ __forceinline__ bool issue_s(Ctrl* ctl, unsigned char* base, const G& geo, Work work, volatile int* abort_flag) {
+// tiles in the current one).
+template <int PAIR, int D, class Work>
+__device__ __forceinline__ bool issue_s(Ctrl* ctl, unsigned char* base, const Geo<PAIR, D>& geo, Work work,
+                                        volatile int* abort_flag) {
+  using G = Geo<PAIR, D>;
   const uint32_t tmem = ctl->tmem_base;
-  const uint32_t idesc = idesc_f32<F16>(128 * PAIR, SPX_TILE_KEYS, false, false);
+  const uint32_t idesc = idesc_bf16_f32(128 * PAIR, SPX_TILE_KEYS, false, false);
   constexpr uint32_t hi = desc_hi(1024);
   const uint32_t q_lo = desc_lo(smem_u32(base), 16), q_blk = geo.q_blk >> 4;
   const uint32_t k_lo = desc_lo(smem_u32(base + geo.k_off), 16);
@@ -249,10 +251,12 @@ __device__ __forceinline__ bool issue_s(Ctrl* ctl, unsigned char* base, const G&
   commit<PAIR>(&ctl->drain);
   return ok;
 }
-template <int PAIR, int D, bool F16 = false, class G, class Work>
-__device__ __forceinline__ bool issue_pv(Ctrl* ctl, unsigned char* base, const G& geo, Work work, volatile int* abort_flag) {
+template <int PAIR, int D, class Work>
+__device__ __forceinline__ bool issue_pv(Ctrl* ctl, unsigned char* base, const Geo<PAIR, D>& geo, Work work,
+                                         volatile int* abort_flag) {
+  using G = Geo<PAIR, D>;
   const uint32_t tmem = ctl->tmem_base, d = tmem + kColO;
-  const uint32_t idesc = idesc_f32<F16>(128 * PAIR, D, false, true);
+  const uint32_t idesc = idesc_bf16_f32(128 * PAIR, D, false, true);
   constexpr uint32_t hi = desc_hi(1024);
   const uint32_t v_lo = desc_lo(smem_u32(base + geo.v_off), PAIR == 2 ? 16 : G::kVBlk);
   int vst = 0, w = 0;

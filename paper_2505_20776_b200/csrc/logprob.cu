@@ -13,7 +13,6 @@
 //
 // What bounds it: reading the logits (HBM), the exponentials (16 a cycle and SM) close behind for bf16; for few rows the chain of
 // latencies: load, reduction, second look, join.
-#include <cstdlib>
 #include "common.cuh"
 #include "pair.cuh"
 
@@ -473,7 +472,6 @@ cudaError_t spx_launch_logprobs(const void* logits, bool f32, int rows, int V, l
   const int words = f32 ? 4 : 8;
   int slices = 1;
   while (slices < kMaxSlices && 2ll * rows * slices <= 4ll * n_sm && V / words >= 2 * slices * 2 * kThreads) slices *= 2;
-  if (getenv("SPX_SL")) slices = atoi(getenv("SPX_SL"));
   a.slices = slices;
   return f32 ? launch<true>(a, rows, st) : launch<false>(a, rows, st);
 }

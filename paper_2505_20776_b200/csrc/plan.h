@@ -19,6 +19,10 @@
 // cluster that merges its results itself: through shared memory, or through the same part of the
 // workspace, where CTA k of problem b then owns entry b * cluster + k ([D/4][128 rows] of float4, and
 // (maximum, row sum) pairs): n_cta entries, no merge kernel.
+//
+// The attention over the 8-bit cache uses the same lines of units.  Kernel 4 has the units above.  Kernel 5, for few rows,
+// cuts the prefix into units of 16 keys and the tree keys into units of 16
+// after them: TPH, UPP, U, q and rem count those, RB is 32 and q_rows, 8 or 16, is the rows of a row block.
 #ifndef SPECEXT_PLAN_H_
 #define SPECEXT_PLAN_H_
 
