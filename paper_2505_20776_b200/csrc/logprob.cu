@@ -5,10 +5,11 @@
 // cluster where rows are few, and joined in the first CTA's shared memory.
 //
 // The best words are found without sorting: a word's key is (logit, lower index first).  Every thread knows its own best key
-// after the pass; the k-th best of the warps' j best thread keys (j times the number of warps >= k) bounds the k-th best key of
-// the CTA from below, so only the vectors of threads with a key that good are looked at again (from L2, all of them
-// dealt to all threads: when each such thread looked through its own, with the rest of its warp waiting, that took longer than
-// the pass), and the few words above the bound are put in order by counting.  Words that are too many for the list (values
+// after the pass (up to its place in a vector); the k-th best of the warps' j best thread keys (j times the number of warps >= k)
+// bounds the k-th best key of the CTA from below, so only threads with a key that good are looked at again: the turn of the
+// loop that had their best, or all their vectors where another turn has a logit that good.  All of it is dealt to all threads (when
+// each such thread looked through its own, with the rest of its warp waiting, that took longer than the pass), and the few
+// words above the bound are put in order by counting.  Words that are too many for the list (values
 // arranged so that one thread has them all) are taken out one by one.
 //
 // What bounds it: reading the logits (HBM), the exponentials (16 a cycle and SM) close behind for bf16; for few rows the chain of
@@ -22,6 +23,7 @@ using namespace pair;
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kNextRow = 32768;
 constexpr int kMaxBest = 32, kMaxSlices = 8, kList = 512;
 constexpr float kLn2 = 0.693147180559945309417f, kLog2e = 1.44269504088896340736f;
 typedef unsigned long long Key;                 // 0: none
@@ -32,7 +34,7 @@ struct LogprobArgs {
   float *logprob, *entropy, *lse, *top_logprob;
   int32_t *top_ids, *status;
   long long stride;
-  int V, given, best, slices;
+  int V, given, best, slices, resident;
   float inv_temperature;
 };
 
@@ -47,7 +49,6 @@ __device__ __forceinline__ Key make_key(float x, int idx) { return ((Key)ordered
 template <bool F32>
 struct Row {
   static constexpr int kWords = F32 ? 4 : 8;
-  static constexpr int kVecs = F32 ? 4 : 2;     // 16-byte loads of a thread at once, and as many for the next turn
   const char* base;                             // of the row, at most 15 bytes below its first word
   int skew, V, n_vec;
   __device__ __forceinline__ Row(const LogprobArgs& a, int row) {
@@ -62,6 +63,7 @@ struct Row {
     return F32 ? *reinterpret_cast<const float*>(at) : __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(at) << 16);
   }
   __device__ __forceinline__ int first_word(int v) const { return v * kWords - skew; }
+  __device__ __forceinline__ int whole() const { return (V + skew) / kWords; }           // vectors up to the last whole one
 };
 
 // Vector v of the row; words outside are -inf.
@@ -91,29 +93,72 @@ __device__ __forceinline__ void unpack(uint4 r, float (&x)[Row<F32>::kWords]) {
     x[j] = F32 ? __uint_as_float(q[j % 4]) : __uint_as_float(j & 1 ? q[j / 2 % 4] & 0xffff0000u : q[j / 2 % 4] << 16);
 }
 
-// Statistics of some words: m their largest logit; with t(x) = x c - m c (c: log2 e / temperature), z the sum of 2^t, e that of
-// 2^t t.  m c is rounded once, and every use rounds it alike, so that it takes no part in the error.  Where even m is a mask (a row
-// of nothing but the type's lowest value), m c might overflow and t is (x - m) c.
+template <bool F32>
+__device__ __forceinline__ uint4 none() {                       // words of -inf
+  constexpr uint32_t q = F32 ? 0xff800000u : 0xff80ff80u;
+  return make_uint4(q, q, q, q);
+}
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {           // (of a number and NaN: the number)
+  uint32_t r;
+  asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// The largest word of a vector.
+template <bool F32>
+__device__ __forceinline__ float largest(uint4 r) {
+  if constexpr (F32) {
+    return fmaxf(fmax3(__uint_as_float(r.x), __uint_as_float(r.y), __uint_as_float(r.z)), __uint_as_float(r.w));
+  } else {
+    const uint32_t m = max_bf16x2(max_bf16x2(r.x, r.y), max_bf16x2(r.z, r.w));
+    return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+  }
+}
+// bf16 words below about -1e30 become that (NaN stays).
+__device__ __forceinline__ uint4 at_least_lowest(uint4 r) {
+  auto lift = [](uint32_t w) {
+    uint32_t q;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(q) : "r"(w), "r"(0xf14af14au));
+    return q;
+  };
+  return make_uint4(lift(r.x), lift(r.y), lift(r.z), lift(r.w));
+}
+
+// Statistics of some words relative to m, their largest logit or one at most kSlack below it: with t(x) = x c - m c (c: log2 e /
+// temperature), z the sum of 2^t, e that of 2^t t.  m c is rounded once, and every use rounds it alike, so that it takes no part in
+// the error.  Where that rounding itself would be large (a row of nothing but masks, which may be the type's lowest value),
+// t is (x - m) c.
 struct Stat {
   float m, z, e;
 };
-constexpr float kMask = -1e36f;
+struct Scale {
+  float c, plain, slack;                        // log2 e / temperature; m below this in magnitude: t is x c - m c; kSlack in logits
+};
+constexpr float kSlack = 4.f;                   // in powers of two
+constexpr float kLarge = 1048576.f;             // of m c: its rounding is 2^-5 and less
+// (temperatures far from any use have every word taken as (x - m) c)
+__device__ __forceinline__ Scale scale_of(float c) {
+  const bool usual = c > 1e-20f && c < 1e6f;
+  return {c, usual ? kLarge / c : 0.f, usual ? kSlack / c : 0.f};
+}
 // `s` relative to a maximum m >= s.m.
-__device__ __forceinline__ Stat at_maximum(Stat s, float m, float c) {
-  const float d = m > kMask ? __fsub_rn(__fmul_rn(s.m, c), __fmul_rn(m, c)) : (s.m - m) * c, f = ex2_approx(d);
+__device__ __forceinline__ Stat at_maximum(Stat s, float m, const Scale& sc) {
+  const bool plain = fabsf(m) < sc.plain, was = fabsf(s.m) < sc.plain;
+  const float to = __fmul_rn(m, sc.c), from = __fmul_rn(s.m, sc.c);
+  const float d = plain ? (was ? __fsub_rn(from, to) : fmaf(s.m, sc.c, -to)) : was ? -fmaf(m, sc.c, -from) : (s.m - m) * sc.c;
+  const float f = ex2_approx(d);
   // (z = 0: no word, or none but -inf; f = 0: nothing is left of it, whatever d is)
   if (s.z == 0.f) return {m, 0.f, 0.f};
   return {m, s.z * f, f == 0.f ? 0.f : f * fmaf(d, s.z, s.e)};
 }
 // The joint statistics of stats[0 .. n), n <= 8, by every warp for itself: a lane has one of them.
-__device__ __forceinline__ Stat join(const Stat* stats, int n, float c) {
+__device__ __forceinline__ Stat join(const Stat* stats, int n, const Scale& sc) {
   const int i = threadIdx.x & 7;
   Stat s = {-INFINITY, 0.f, 0.f};
   if (i < n) s = stats[i];
   float m = s.m;
 #pragma unroll
   for (int o = 1; o < 8; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  s = at_maximum(s, m, c);
+  s = at_maximum(s, m, sc);
 #pragma unroll
   for (int o = 1; o < 8; o <<= 1) {
     s.z += __shfl_xor_sync(0xffffffffu, s.z, o);
@@ -129,7 +174,7 @@ struct Shared {
   Key list[kList];
   Key top[kMaxBest];
   int n_list, n_again;
-  unsigned char again[kThreads];                // threads whose vectors are looked at again
+  int again[kThreads];                          // what is looked at again: a turn's first vector, or -1 - thread: all its vectors
   // in the first CTA of a cluster, from all of it
   Stat stat[kMaxSlices];
   Key keys[kMaxSlices * kMaxBest];
@@ -155,6 +200,14 @@ __device__ __forceinline__ void in_order(const Key* keys, int n, Put&& put) {
   }
 }
 
+// `n` vectors from v on to L2, as far as they lie before `end`.
+template <bool F32>
+__device__ __forceinline__ void prefetch_l2(const Row<F32>& row, int v, int n, int end) {
+  n = min(n, end - v);
+  if (n > 0)
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(row.base + (long long)v * 16), "r"(n * 16) : "memory");
+}
+
 // use(key) for every word of vector v (NaN has none).
 template <bool F32, class Use>
 __device__ __forceinline__ void each_key(const Row<F32>& row, int v, Use&& use) {
@@ -168,10 +221,10 @@ __device__ __forceinline__ void each_key(const Row<F32>& row, int v, Use&& use) 
   }
 }
 
-// The `best` best keys of the words in vectors [lo, hi) to sh.top, in order (zeros where there are no more words), from the
-// threads' best keys; `full` warps had a vector for every thread, and their best thread keys are in sh.bounds.
+// The `best` best keys of the words in vectors [lo, hi) to sh.top, in order (zeros where there are no more words).  `mine`: no word
+// of the thread has a better key; `full` warps had a vector for every thread, and their best thread keys are in sh.bounds.
 template <bool F32>
-__device__ __forceinline__ void best_words(Shared& sh, const Row<F32>& row, int lo, int hi, int best, Key mine, int full) {
+__device__ __forceinline__ void best_words(Shared& sh, const Row<F32>& row, int lo, int hi, int best, Key mine, int turn, int n_turn, Key rest, int full) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   // The bound: of the warps' best thread keys (j of each, at least k in all) the k-th best; or the lowest, where they are too many
   // for a warp to look at.
@@ -189,19 +242,19 @@ __device__ __forceinline__ void best_words(Shared& sh, const Row<F32>& row, int 
     bound = sh.bounds[j - 1];
     for (int i = 1; i < full; ++i) bound = min(bound, sh.bounds[i * j + j - 1]);
   }
-  if (mine != 0 && mine >= bound) sh.again[atomicAdd(&sh.n_again, 1)] = (unsigned char)tid;
+  if (mine != 0 && mine >= bound) sh.again[atomicAdd(&sh.n_again, 1)] = rest >= bound ? -1 - tid : turn;
   __syncthreads();
-  const int per = (hi - lo + kThreads - 1) / kThreads, n_again = sh.n_again;
-  // 8 to 32 threads to each of those threads' vectors
-  const int log_team = per > 16 ? 5 : per > 8 ? 4 : 3, member = tid & ((1 << log_team) - 1);
-  for (int q = tid >> log_team; q < n_again; q += kThreads >> log_team)
-    for (int v = lo + sh.again[q] + member * kThreads; v < hi; v += kThreads << log_team)
+  const int n_again = sh.n_again, member = tid & 7;        // 8 threads to each
+  for (int q = tid >> 3; q < n_again; q += kThreads >> 3) {
+    const int what = sh.again[q], first = what < 0 ? lo - 1 - what : what, end = what < 0 ? hi : min(hi, first + n_turn);
+    for (int v = first + member * kThreads; v < end; v += 8 * kThreads)
       each_key(row, v, [&](Key k) {
         if (k >= bound) {
           const int at = atomicAdd(&sh.n_list, 1);
           if (at < kList) sh.list[at] = k;
         }
       });
+  }
   __syncthreads();
   const int n = sh.n_list;
   if (n <= kList) {
@@ -229,9 +282,14 @@ __device__ __forceinline__ void best_words(Shared& sh, const Row<F32>& row, int 
   __syncthreads();
 }
 
-template <bool F32>
+// AHEAD: more rows than CTAs at once, so that reading is what counts: two turns ahead go to L2, and the next row's beginning while this
+// one's words are put in order.  us per call with / without: 2047 rows of 32000 fp32 53.3 / 58.6, bf16 42.5 / 45.6, 1500 of 128256 bf16
+// 86 / 93; 200 of 32000 fp32 13.2 / 11.2, 500 of 128256 bf16 38 / 36.9.  (128 threads and twice the CTAs: 56.9 and 39.4 of the first and last.)
+template <bool F32, bool AHEAD>
 __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(const __grid_constant__ LogprobArgs a) {
-  constexpr int W = Row<F32>::kWords, kVecs = Row<F32>::kVecs;
+  constexpr int W = Row<F32>::kWords;
+  constexpr int kVecs = F32 || AHEAD ? 4 : 2;   // 16-byte loads of a thread at once, and as many for the next turn
+  constexpr int kTurn = kVecs * kThreads;
   __shared__ Shared sh;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int n_slices = a.slices, r = (int)blockIdx.x / n_slices, rank = (int)blockIdx.x - r * n_slices;
@@ -253,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(const __grid_const
   const Row<F32> row(a, r);
   const int per = (row.n_vec + n_slices - 1) / n_slices;
   const int lo = min(row.n_vec, rank * per), hi = min(row.n_vec, lo + per);
-  const float c = a.inv_temperature * kLog2e;
+  const Scale sc = scale_of(a.inv_temperature * kLog2e);
   pdl_wait();
   // the first given tokens' logits, ahead of the pass
   int token = -1;
@@ -263,85 +321,95 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(const __grid_const
     if (token >= 0 && token < a.V) given = row.word(token);
   }
 
+  // Of a thread: its best logit, the first vector that has it, and the best logit of the other turns of its loop.
   Stat s = {-INFINITY, 0.f, 0.f};
-  float top_value = -INFINITY;
-  int top_v = -1;
-  uint4 top_raw = make_uint4(0u, 0u, 0u, 0u);
+  float top_value = -INFINITY, other = -INFINITY;
+  int top_v = lo + tid;
   uint4 next[kVecs];
+  const int in_lo = max(lo, row.skew > 0 ? 1 : 0), in_hi = min(hi, row.whole());        // vectors without words outside
   auto fetch = [&](int v) {
+    if (v >= in_lo && v + (kVecs - 1) * kThreads < in_hi) {
+      const uint4* at = reinterpret_cast<const uint4*>(row.base) + v;
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i)
-      next[i] = v + i * kThreads < hi ? load_vec(row, v + i * kThreads)
-                                      : (F32 ? make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u)
-                                             : make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u));
+      for (int i = 0; i < kVecs; ++i) next[i] = at[i * kThreads];
+    } else {
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i)
+        next[i] = v + i * kThreads < hi ? load_vec(row, v + i * kThreads) : none<F32>();
+    }
   };
   fetch(lo + tid);
-  const uint64_t c2 = pack_f32x2(c, c);
-  for (int v = lo + tid; v < hi; v += kVecs * kThreads) {
+  if (AHEAD && tid == 0) prefetch_l2(row, lo + kTurn, kTurn, in_hi);
+  const uint64_t c2 = pack_f32x2(sc.c, sc.c);
+  for (int v = lo + tid; v < hi; v += kTurn) {
     uint4 raw[kVecs];
     float x[kVecs][W], vm[kVecs], m = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) raw[i] = next[i];
-    if (v + kVecs * kThreads < hi) fetch(v + kVecs * kThreads);
+    if (v + kTurn < hi) fetch(v + kTurn);
+    if (AHEAD && tid == 0) prefetch_l2(row, v + 2 * kTurn, kTurn, in_hi);
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-      unpack<F32>(raw[i], x[i]);
-      vm[i] = fmaxf(x[i][0], x[i][1]);
-#pragma unroll
-      for (int j = 2; j < W; j += 2) vm[i] = fmax3(vm[i], x[i][j], x[i][j + 1]);
+      vm[i] = largest<F32>(raw[i]);
       m = fmaxf(m, vm[i]);
     }
-    if (m > top_value || top_v < 0) {
+    other = fmaxf(other, fminf(m, top_value));
+    if (m > top_value) {
       top_value = m;
       top_v = v;
-      top_raw = raw[0];
 #pragma unroll
-      for (int i = kVecs - 1; i > 0; --i)       // (the first vector that has the maximum, and that exists)
-        if (vm[i] == m && vm[0] != m) {
-          top_v = v + i * kThreads;
-          top_raw = raw[i];
-        }
+      for (int i = kVecs - 1; i > 0; --i)
+        if (vm[i] == m && vm[0] != m) top_v = v + i * kThreads;
     }
-    if (m > s.m) s = at_maximum(s, m, c);
-    if (s.m > kMask) {
-      const float neg = -__fmul_rn(s.m, c);
+    // a new reference only where the sums would grow large: a maximum that only just rises is most turns' case for some thread of a warp
+    if (m > s.m + sc.slack) s = at_maximum(s, m, sc);
+    const float ref = s.m == -INFINITY ? 0.f : s.m;       // (nothing but -inf and NaN so far)
+    if (fabsf(ref) < sc.plain) {
+      const float neg = -__fmul_rn(ref, sc.c);
       const uint64_t neg2 = pack_f32x2(neg, neg);
       uint64_t z = 0ull, e = 0ull;
 #pragma unroll
-      for (int i = 0; i < kVecs; ++i)
+      for (int i = 0; i < kVecs; ++i) {
+        // (a word masked out: 0 times a large number, not times infinity)
+        unpack<F32>(F32 ? raw[i] : at_least_lowest(raw[i]), x[i]);
 #pragma unroll
         for (int j = 0; j < W; j += 2) {
           float t0, t1;
           unpack_f32x2(fma_f32x2(pack_f32x2(x[i][j], x[i][j + 1]), c2, neg2), t0, t1);
           const uint64_t q = pack_f32x2(ex2_approx(t0), ex2_approx(t1));
           z = add_f32x2(z, q);
-          // (a word masked out: 0 times a large number, not times infinity)
-          e = fma_f32x2(q, pack_f32x2(fmaxf(t0, -1e30f), fmaxf(t1, -1e30f)), e);
+          e = fma_f32x2(q, F32 ? pack_f32x2(fmaxf(t0, -1e30f), fmaxf(t1, -1e30f)) : pack_f32x2(t0, t1), e);
         }
+      }
       float z0, z1, e0, e1;
       unpack_f32x2(z, z0, z1);
       unpack_f32x2(e, e0, e1);
       s.z += z0 + z1;
       s.e += e0 + e1;
     } else {
-      // nothing but masks and NaN so far: word by word
-      const float m0 = s.m == -INFINITY ? 0.f : s.m;
-#pragma unroll 1
-      for (int i = 0; i < kVecs * W; ++i) {
-        const int u = v + i / W * kThreads, idx = row.first_word(u) + i % W;
-        if (u >= hi || idx < 0 || idx >= row.V) continue;
-        const float t = (row.word(idx) - m0) * c, q = ex2_approx(t);
-        s.z += q;
-        s.e = fmaf(q, fmaxf(t, -1e30f), s.e);
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i) {
+        unpack<F32>(raw[i], x[i]);
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+          const float t = (x[i][j] - ref) * sc.c, q = ex2_approx(t);
+          s.z += q;
+          s.e = fmaf(q, fmaxf(t, -1e30f), s.e);
+        }
       }
     }
   }
 
+  // the beginning of the row that this place on the SM will most likely have next, while nothing else is read
+  if (AHEAD && tid == 0 && blockIdx.x + a.resident < gridDim.x) {
+    const Row<F32> later(a, blockIdx.x + a.resident);
+    prefetch_l2(later, 0, kNextRow / 16, later.whole());
+  }
   // warp: statistics, and the j-th best of its threads' best keys
-  float m = s.m;
+  float m = top_value;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  s = at_maximum(s, m, c);
+  s = at_maximum(s, m, sc);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     s.z += __shfl_xor_sync(0xffffffffu, s.z, o);
@@ -351,17 +419,10 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(const __grid_const
   const int full = min(kWarps, (hi - lo) / 32);           // warps with a vector for every thread
   Key mine = 0;
   if (a.best > 0) {
-    if (top_v >= 0) {
-      float x[W];
-      unpack<F32>(top_raw, x);
-#pragma unroll
-      for (int j = W - 1; j >= 0; --j) {
-        const int idx = row.first_word(top_v) + j;
-        if (x[j] == top_value && idx >= 0 && idx < row.V) mine = make_key(x[j], idx);
-      }
-    }
+    // its best word is one of vector top_v: at least as good as `k` below, at most as good as `mine`
+    if (top_v < hi) mine = make_key(top_value, max(row.first_word(top_v), 0));
     if (warp < full) {
-      Key k = mine;
+      Key k = top_v < hi ? make_key(top_value, row.first_word(top_v) + W - 1) : 0;
       const int j = (a.best + full - 1) / full;
 #pragma unroll 1
       for (int i = 0; i < j; ++i) {
@@ -372,8 +433,11 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(const __grid_const
     }
   }
   __syncthreads();
-  s = join(sh.warp_stat, kWarps, c);
-  if (a.best > 0) best_words(sh, row, lo, hi, a.best, mine, full);
+  s = join(sh.warp_stat, kWarps, sc);
+  if (a.best > 0) {
+    const int turn = lo + tid + (top_v - lo - tid) / kTurn * kTurn;
+    best_words(sh, row, lo, hi, a.best, mine, turn, kTurn, make_key(other, 0), full);
+  }
 
   const Key* keys = sh.top;
   int n_keys = a.best;
@@ -398,7 +462,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(const __grid_const
       settle();
       return;
     }
-    s = join(sh.stat, n_slices, c);
+    s = join(sh.stat, n_slices, sc);
     keys = sh.keys;
     n_keys = n_slices * a.best;
   }
@@ -406,7 +470,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(const __grid_const
   // log(z) of a row without a finite logit is -inf: all its log probabilities are, and its entropy is 0
   const bool empty = s.z == 0.f;
   // log Z relative to m itself: what m c was rounded by is put right
-  const float log2_z = log2f(s.z), off = s.m > kMask ? fmaf(s.m, c, -__fmul_rn(s.m, c)) : 0.f;
+  const float log2_z = log2f(s.z), off = fabsf(s.m) < sc.plain ? fmaf(s.m, sc.c, -__fmul_rn(s.m, sc.c)) : 0.f;
   const float log_z = (log2_z - off) * kLn2, lse = empty ? -INFINITY : fmaf(s.m, a.inv_temperature, log_z);
   // (the difference to the maximum first: x - lse would lose log Z where the maximum is huge, as in a row of the type's lowest value)
   auto log_p = [&](float raw) { return empty ? -INFINITY : fmaf(raw - s.m, a.inv_temperature, -log_z); };
@@ -439,7 +503,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(const __grid_const
   }
 }
 
-template <bool F32>
+template <bool F32, bool AHEAD>
 cudaError_t launch(const LogprobArgs& a, int rows, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)rows * (unsigned)a.slices);
@@ -454,7 +518,7 @@ cudaError_t launch(const LogprobArgs& a, int rows, cudaStream_t st) {
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = a.slices > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, logprob_kernel<F32>, a);
+  return cudaLaunchKernelEx(&cfg, logprob_kernel<F32, AHEAD>, a);
 }
 
 }  // namespace
@@ -473,5 +537,7 @@ cudaError_t spx_launch_logprobs(const void* logits, bool f32, int rows, int V, l
   int slices = 1;
   while (slices < kMaxSlices && 2ll * rows * slices <= 4ll * n_sm && V / words >= 2 * slices * 2 * kThreads) slices *= 2;
   a.slices = slices;
-  return f32 ? launch<true>(a, rows, st) : launch<false>(a, rows, st);
+  a.resident = 4 * n_sm;
+  if (rows > a.resident) return f32 ? launch<true, true>(a, rows, st) : launch<false, true>(a, rows, st);
+  return f32 ? launch<true, false>(a, rows, st) : launch<false, false>(a, rows, st);
 }

@@ -29,6 +29,9 @@ def _check(logits, tokens, k, temperature=1.0):
     np.testing.assert_array_equal(ids.cpu().numpy(), r_ids)
     size = np.max(np.abs(x[np.isfinite(x)]), initial=0.0) / temperature if np.isfinite(x).any() else 0.0
     size = min(size, 1e6)                                            # (the type's lowest value as a mask takes no part)
+    # (results are fp32: bf16's lowest value / 0.7 is -4.84e38, past its range of 3.41e38, and rounds to -inf)
+    with np.errstate(over="ignore"):
+        r_lse = np.asarray(r_lse).astype(np.float32).astype(np.float64)
     np.testing.assert_allclose(f64(lse), r_lse, rtol=1e-6, atol=2e-6)
     np.testing.assert_allclose(f64(ent), r_ent, rtol=1e-6, atol=4e-6)
     np.testing.assert_allclose(f64(top), r_top, rtol=1e-6, atol=2e-6 + 2.0 ** -22 * size)
@@ -152,3 +155,60 @@ def test_the_same_call_gives_the_same_bits(cuda_device):
         ref = hp.token_logprobs(x, None, 20)[1:]
         for _ in range(20):
             assert all(torch.equal(a, b) for a, b in zip(ref, hp.token_logprobs(x, None, 20)[1:]))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_more_rows_than_run_at_once(cuda_device, dtype):
+    """Odd row strides, and rows of masks, ties, one place, NaN and +inf among them."""
+    dev, R, V = cuda_device, 640, 9001
+    x = _logits(R, V, dtype, dev, 11, V + 2, 3)
+    x[0], x[1], x[2] = float("-inf"), torch.finfo(dtype).min, 0
+    x[3, 1:] = float("-inf")
+    x[600, 4000:] = torch.finfo(dtype).min
+    x[601, :] = torch.arange(V, device=dev).to(dtype) / 512
+    x[602, 77], x[603, 8000] = float("nan"), float("inf")
+    x[R - 1, : V - 3] = float("-inf")
+    _check(x, np.random.default_rng(3).integers(-1, V, (R, 2)), 24, 0.7)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("mask", [-1e4, -7.2e5, -7.3e5, -0.9e29, -1.1e29, -1e30, -3e38])
+def test_masks_of_any_size(cuda_device, dtype, mask):
+    """Rows with few words left, none (each word as likely as the next), or two levels of masks; the sums change their form at 2^20 / c."""
+    dev, V = cuda_device, 20003
+    x = _logits(5, V, dtype, dev, 12).clone()
+    keep = x[:, [9, 12345, V - 1]].clone()
+    x[0] = x[1] = x[2] = mask
+    x[0, [9, 12345, V - 1]] = keep[0]
+    x[1, 12345] = 0
+    x[3, : V // 2] = mask
+    x[4] = mask
+    x[4, ::3] = float("-inf")
+    _check(x, [[9, 0], [12345, 1], [5, 6], [0, V - 1], [0, 1]], 8)
+
+
+@pytest.mark.parametrize("temperature", [1e-3, 30.0, 1e9, 1e25])
+def test_temperatures(cuda_device, temperature):
+    for dtype in (torch.bfloat16, torch.float32):
+        x = _logits(3, 7001, dtype, cuda_device, 13).clone()
+        x[2, ::2] = float("-inf")
+        _check(x, [[0], [1], [2]], 6, temperature)
+
+
+def test_references_that_rise_all_along(cuda_device):
+    """Every turn of every thread brings a larger maximum: by less than a rescaling takes, by just as much, and by far more."""
+    dev, V = cuda_device, 40000
+    turn = torch.arange(V, device=dev, dtype=torch.float32) / 2048
+    x = torch.stack([turn * 0.2, turn * 4 * 0.6931472, turn * 40, -turn * 0.2])
+    _check(x, [[0], [V - 1], [V // 2], [3]], 12)
+    _check(x.to(torch.bfloat16), [[0], [V - 1], [V // 2], [3]], 12)
+
+
+def test_maxima_on_both_sides_of_the_change_of_form(cuda_device):
+    """Logits around -2^20 / c and 2^20 / c, a few units wide: threads with the one form are joined with threads with the other."""
+    dev, V = cuda_device, 30000
+    at = 2.0 ** 20 * 0.6931471805599453
+    g = torch.Generator().manual_seed(14)
+    wide = (torch.rand((2, V), generator=g, dtype=torch.float64) * 6 - 3).to(dev)
+    wide[:, : V // 2] += torch.arange(V // 2, device=dev) * (4.0 / V)
+    _check(torch.stack([wide[0] - at, wide[1] + at]).float(), [[0], [V - 1]], 12)
