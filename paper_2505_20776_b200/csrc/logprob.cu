@@ -531,13 +531,13 @@ cudaError_t spx_launch_logprobs(const void* logits, bool f32, int rows, int V, l
   a.logprob = logprob; a.entropy = entropy; a.lse = lse; a.top_ids = top_ids; a.top_logprob = top_logprob; a.status = status;
   a.stride = stride; a.V = V; a.given = given; a.best = best; a.inv_temperature = inv_temperature;
   // CTAs per row: as many as are resident at once (four per SM), as long as a thread has two vectors and more.  us per call, 1 / 2 /
-  // 4 / 8: one row of 32000 bf16 7.9 / 6.3 / 5.6 / 5.7, 16 of 128256 34 / 20 / 13 / 10, 60 of 128256 38 / 24 / 19 / 15, 200 of 32000
-  // fp32 17.0 / 13.8 / 16.8 / 23.0, 2047 of 32000 69 / 87 / 122 / 191
+  // 4 / 8: one row of 32000 bf16 6.6 / 5.8 / 5.3 / 5.4, 16 of 128256 27 / 15.7 / 10.4 / 8.7, 60 of 128256 28 / 16.8 / 13.5 / 10.8, 200 of
+  // 32000 fp32 12.6 / 11.2 / 15.3 / 22.9
   const int words = f32 ? 4 : 8;
   int slices = 1;
   while (slices < kMaxSlices && 2ll * rows * slices <= 4ll * n_sm && V / words >= 2 * slices * 2 * kThreads) slices *= 2;
   a.slices = slices;
   a.resident = 4 * n_sm;
-  if (rows > a.resident) return f32 ? launch<true, true>(a, rows, st) : launch<false, true>(a, rows, st);
+  if (slices == 1 && rows > a.resident) return f32 ? launch<true, true>(a, rows, st) : launch<false, true>(a, rows, st);
   return f32 ? launch<true, false>(a, rows, st) : launch<false, false>(a, rows, st);
 }
