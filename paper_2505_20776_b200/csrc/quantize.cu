@@ -5,7 +5,8 @@
 // the ratio of both, a power of two, which rounds only what falls among e4m3's subnormals.
 //
 // What bounds it: memory for prompts, latency for the few tokens of a decoding step.  A thread block has one block of one head
-// of K or V, all of it in registers between the maximum and the rounding, so everything is read and written once.
+// of K or V, all of it in registers between the maximum and the rounding, so everything is read and written once.  Replayed, 8 heads
+// of 128: 60 tokens 1.8 us, 2000 4.9, 16384 17.4 (5.8 TB/s of reads and writes), 131072 117 (6.9).
 #include "q8.cuh"
 #include "sm100.cuh"
 
