@@ -283,7 +283,8 @@ __device__ __forceinline__ float4 join_warps(const float* o, const float2 (&ml)[
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
   for (int i = 0; i < kWarps; ++i) {
-    const float f = ex2_approx(w[i] - m);
+    // (none: no key of the warp is seen by the row, nor of any other where m is none too, as in a worker that has later tree keys only)
+    const float f = w[i] == -INFINITY ? 0.f : ex2_approx(w[i] - m);
     const float4 x = *reinterpret_cast<const float4*>(o + (i * ROWS + row) * D + ((col ^ (row >> 1 & 3)) << 2));
     l = fmaf(ml[i][row].y, f, l);
     acc.x = fmaf(f, x.x, acc.x);

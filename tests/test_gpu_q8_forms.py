@@ -106,3 +106,20 @@ def test_values_that_are_not_finite_stay_with_their_rows(cuda_device, T, L, valu
     else:
         # an infinite logit: NaN, or the key's weight is 0 or 1; never a finite stand-in for the infinity
         assert torch.equal(hp.O[hit].isnan().any(dim=1), hp.O[hit].isnan().all(dim=1))
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,T,L", [(4, 4, 128, 100, 32), (4, 4, 128, 128, 16), (4, 4, 64, 128, 160), (8, 4, 128, 100, 32),
+                                          (2, 2, 128, 128, 0), (2, 1, 64, 65, 70)])
+def test_workers_that_have_only_tree_keys_behind_a_row(cuda_device, Hq, Hkv, D, T, L):
+    """Large trees on short prefixes: some workers have no key that the first nodes see."""
+    dev = cuda_device
+    c = _filled(Hkv, D, max(L, 1), 32, dev, T + L)
+    c.length = L
+    hp = GuardedHotPath(Hq, Hkv, D, T, 32, 4, max(L, 1), device=dev)
+    t = _tensors(Hq, Hkv, D, T, dev, L)
+    parent = random_forest(np.random.default_rng(L), T)
+    hp.verify_attn_q8(t, c, torch.from_numpy(parent).to(dev), False)
+    assert hp.read_status() == 0
+    hp.check()
+    K, V = values(c, L)
+    check_attention(t["Q"], K, V, t["K_tree"], t["V_tree"], parent, 32, hp.O, hp.lse, None)
