@@ -38,6 +38,7 @@ class HotPath:
         self.K_compact = self._alloc(shape, torch.bfloat16).zero_()
         self.V_compact = self._alloc(shape, torch.bfloat16).zero_()
         self._ws = self._alloc((0,), torch.uint8)
+        self._ws_q8 = [self._ws]
 
     # -- helpers -------------------------------------------------------------------------------
     def _alloc(self, shape, dtype) -> torch.Tensor:
@@ -80,11 +81,14 @@ class HotPath:
         need = api.specext_verify_attn_q8_workspace(d, cache.block_tokens)
         if need == 0:
             raise api.SpecextError(2, "specext_verify_attn_q8_workspace")
-        if self._ws.numel() < need:
-            self._ws = self._alloc((need,), torch.uint8)
+        if self._ws_q8[-1].numel() < need:
+            # for all prefixes up to the longest at once; outgrown ones stay, since a captured graph may still write to them
+            longest = api.make_attn_desc(t["Q"], cache.K, t["K_tree"], self.O, self.max_prefix, self.C, self.scale, want_score)
+            need = max(need, api.specext_verify_attn_q8_workspace(longest, cache.block_tokens))
+            self._ws_q8.append(self._alloc((need,), torch.uint8))
         api.specext_verify_attn_q8(d, t["Q"], cache.K, cache.V, cache.K_scale, cache.V_scale, cache.block_tokens, t["K_tree"],
-                                   t["V_tree"], parent, self.O, self.lse, self._score_flat if want_score else None, self._ws,
-                                   self.status)
+                                   t["V_tree"], parent, self.O, self.lse, self._score_flat if want_score else None,
+                                   self._ws_q8[-1], self.status)
 
     def token_logprobs(self, logits: torch.Tensor, tokens: Optional[torch.Tensor], n_best: int, temperature: float = 1.0
                        ) -> Tuple[Optional[torch.Tensor], torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:

@@ -200,3 +200,31 @@ def test_on_another_stream_beside_other_work(cuda_device):
         assert s[0].read_status() == 0 and s[1].read_status() == 0
         s[0].check()
         s[1].check()
+
+
+def test_a_graph_keeps_its_workspace(cuda_device):
+    """A graph of a call with a small workspace is replayed after calls that need larger ones."""
+    dev, L = cuda_device, 6001
+    g = torch.Generator().manual_seed(21)
+    cache = GuardedCache8(HKV, D, L, 32, dev)
+    cache.append(*(torch.randn((L, HKV, D), generator=g).to(torch.bfloat16).to(dev) for _ in range(2)))
+    hp = GuardedHotPath(HQ, HKV, D, T, C, K_TOP, L, device=dev)
+    t, parent, _, _ = _inputs(dev, 22)
+    par = torch.from_numpy(parent).to(dev)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        hp.verify_attn_q8(t, cache, par, False)
+    torch.cuda.synchronize()
+    want, graph = hp.O.clone(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        hp.verify_attn_q8(t, cache, par, False)
+    captured = hp._ws_q8[-1]
+    hp.verify_attn_q8(t, cache, par, True)
+    assert hp._ws_q8[-1] is not captured and any(w is captured for w in hp._ws_q8)
+    hp.O.zero_()
+    torch.cuda.synchronize()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert hp.read_status() == 0 and torch.equal(hp.O, want)
+    hp.check()
