@@ -149,7 +149,9 @@ int specext_quantize_kv(const void* K, const void* V, int32_t n_src, int32_t n_k
  * their 32 nodes (those 2^-10 of it and less are kept to 2^-18 of it, for up to 16 rows per KV head to 2^-39) and are
  * accumulated in fp32; probabilities, times the V scale, are rounded to f16 for the product with V (11 bits;
  * 2^-30 and less of a row's largest counts as zero); chunk sums and the normaliser are accumulated in fp32 from
- * unrounded exponentials.  Everything else as in specext_verify_attn, chunk_score included, so that
+ * unrounded exponentials.  V's scale is part of the exponent: where the V scales of a head's blocks (2^-100 for a block of
+ * zeros) lie 2^d apart, d > 100, weights of 2^(d-132) of the largest and less are lost in the blocks of the lowest (2^-30 and
+ * less at d = 102).  Everything else as in specext_verify_attn, chunk_score included, so that
  * SelectChunks and UpdateDraftCache follow unchanged.  The workspace has a size of its own.
  */
 size_t specext_verify_attn_q8_workspace(const specext_attn_desc* desc, const specext_q8_desc* q8);

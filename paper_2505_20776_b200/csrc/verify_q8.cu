@@ -16,8 +16,8 @@
 // (First both K and V were expanded to f16, by the same four warps: 2.7 us a tile of 128 keys against 0.75 for its bytes.)
 //
 // Warps: 0-7 the queries' parts, then softmax; 8 TMA producer of the codes, 9 issuer of the S MMAs, 10 of the PV MMAs, 11
-// ancestor masks and TMA producer of Q, 12-15 expansion (V: a thread has a key; the tree's keys and values).  Every wait is bounded; all threads
-// reach the final barrier before tensor memory is freed.
+// ancestor masks, TMA producer of Q and the tree's keys and values, 12-15 expansion of V (a thread has a key).  Every wait is bounded; all
+// threads reach the final barrier before tensor memory is freed.
 #include "core.cuh"
 #include "q8.cuh"
 #include "tmap.h"
@@ -66,8 +66,10 @@ struct CtrlQ8 {
   uint64_t vc_full[kMaxUnits], vc_empty[kMaxUnits];      // this CTA: codes of V, between the producer and the expansion
   uint64_t q_land, q_read;                     // this CTA: the bf16 queries have landed; 8 warps have read them
   uint64_t q_ready;                            // leader: 8 warps per CTA have made their query rows
-  uint64_t sc_ready;                           // this CTA: the scales of the run's prefix tiles are in shared memory
-  int tree_k[4], tree_v[4];                    // exponents of the tree's groups
+  uint64_t sc_ready;                           // this CTA: the scales of the run's tiles are in shared memory
+  uint64_t tree_go;                            // this CTA: the expansion is two tiles from the end of the prefix
+  int tree_k[4], tree_v[4];                    // exponents of the tree's groups of 32 nodes
+  uint2 tree_max[4][4];                        // largest magnitudes of K and V of a group, a quarter of the nodes each
   float q_scale[128];
 };
 constexpr int kCtrlBytesQ8 = 7168;
@@ -212,15 +214,11 @@ __device__ __forceinline__ void split16(uint4 x, uint4 y, float f, unsigned char
   *reinterpret_cast<uint4*>(lo) = l;
 }
 
-// The largest finite magnitude in the rows of a warp's 32 tree nodes (a lane has one).
-template <int D>
-__device__ __forceinline__ uint32_t tree_amax(const __nv_bfloat16* src, bool valid) {
-  uint32_t m = 0u;
-  const uint4* row = reinterpret_cast<const uint4*>(src);
-#pragma unroll 4
-  for (int c = 0; c < D / 8; ++c) m = amax_bf16x8(m, valid ? row[c] : make_uint4(0u, 0u, 0u, 0u));
-  return __reduce_max_sync(0xffffffffu, m);
+// 16 bytes of a tree node's row into shared memory, or zeros.
+__device__ __forceinline__ void copy_node(unsigned char* dst, const __nv_bfloat16* src, bool in) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(in ? 16u : 0u) : "memory");
 }
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // Issuers of the S and of the PV MMAs (issue_s and issue_pv of core.cuh for one run of tiles, by whole warps of the leader CTA).
 // has_tree: the last tile of the run is the tree's, two units of K.
@@ -444,6 +442,7 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
       mbar_init(&ctl8->q_land, 1);
       mbar_init(&ctl8->q_read, 8);
       mbar_init(&ctl8->sc_ready, 4);
+      mbar_init(&ctl8->tree_go, 1);
       mbar_init(&ctl8->q_ready, 8 * PAIR);
     }
     fence_mbar_init();
@@ -457,6 +456,39 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
     setmaxnreg_dec<kRegsOtherQ8>();
     const int group = warp - kExpandWarp, key = group * 32 + lane;
     pdl_wait();
+    if (has_tree) {
+      const __nv_bfloat16 *kt = a.Kt + (long long)g * a.tkv_sh, *vt = a.Vt + (long long)g * a.tkv_sh;
+      // scales of the tree, a quarter of every group's nodes a warp, ahead of the keys' and values' copies as far as may be
+      constexpr int kLanes = D / 8, kStep = 32 / kLanes;
+#pragma unroll 1
+      for (int q = 0; q * 32 < p.T; ++q) {
+        uint32_t km = 0u, vm = 0u;
+#pragma unroll
+        for (int i = 0; i < 8; i += kStep) {
+          const int node = q * 32 + group * 8 + i + lane / kLanes;
+          const long long at = (long long)node * a.tkv_st + (lane % kLanes) * 8;
+          const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+          km = amax_bf16x8(km, node < p.T ? *reinterpret_cast<const uint4*>(kt + at) : none);
+          vm = amax_bf16x8(vm, node < p.T ? *reinterpret_cast<const uint4*>(vt + at) : none);
+        }
+        km = __reduce_max_sync(0xffffffffu, km);
+        vm = __reduce_max_sync(0xffffffffu, vm);
+        if (lane == 0) ctl8->tree_max[q][group] = make_uint2(km, vm);
+      }
+      named_bar_sync(1, 128);
+      if (key < 4) {
+        uint2 m = make_uint2(0u, 0u);
+        if (key * 32 < p.T)
+          for (int i = 0; i < 4; ++i) m = make_uint2(max(m.x, ctl8->tree_max[key][i].x), max(m.y, ctl8->tree_max[key][i].y));
+        const int ke = e4m3_exponent(m.x), ve = f16_exponent(m.y);
+        ctl8->tree_k[key] = ke;
+        ctl8->tree_v[key] = ve;
+        Q8Scales* sc = scales + n_pref;
+        reinterpret_cast<float*>(&sc->k)[key] = exp2_int(ke);
+        reinterpret_cast<float*>(&sc->v_log2)[key] = (float)ve;
+        reinterpret_cast<float*>(&sc->v_inv)[key] = exp2_int(-ve);
+      }
+    }
     // scales of the run: a thread has a group of a tile (groups behind the prefix have no key and any scale)
     for (int i = key; i < n_pref * 4; i += 128) {
       const int token = min((tile_lo + (i >> 2)) * SPX_TILE_KEYS + (i & 3) * 32, p.L - 1);
@@ -468,12 +500,14 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
       reinterpret_cast<float*>(&sc->v_inv)[i & 3] = e8m0_value(vcode == 255u ? 255u : 254u - vcode);
     }
     warp_arrive(&ctl8->sc_ready, lane);
-    ok = mbar_wait(&ctl8->q_read, 0, abort_flag);        // (they lie where V's stages will be)
+    ok = mbar_wait(&ctl8->q_read, 0, abort_flag) && mbar_wait(&ctl8->sc_ready, 0, abort_flag);        // (they lie where V's stages will be)
     int vc = 0, vst = 0;
     uint32_t vcph = 0, vph = 1;
+    if (n_pref < 2 && key == 0) mbar_arrive(&ctl8->tree_go);
     for (int j = 0; j < n_pref && ok; ++j) {
       ok = mbar_wait(&ctl8->vc_full[vc], vcph, abort_flag) && wait_c(&ctl->v_empty[vst], vph, abort_flag);
       if (!ok) break;
+      if (j == n_pref - 2 && key == 0) mbar_arrive(&ctl8->tree_go);
       expand_key<G::kVRow>(base + G::v8_off + vc * G::kVUnit, base + G::v_off + vst * G::kVStage, key);
       publish<PAIR>(&ctl->v_full[vst], lane);
       if (lane == 0) mbar_arrive(&ctl8->vc_empty[vc]);
@@ -486,59 +520,24 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
         vph ^= 1;
       }
     }
-    if (has_tree) {
-      // (no early way out: the meetings below are everybody's)
-      const __nv_bfloat16* kt = a.Kt + (long long)g * a.tkv_sh;
-      const __nv_bfloat16* vt = a.Vt + (long long)g * a.tkv_sh;
-      const uint4 none = make_uint4(0u, 0u, 0u, 0u);
-      {
-        const bool node = key < p.T;
-        const uint32_t km = tree_amax<D>(kt + (long long)key * a.tkv_st, node), vm = tree_amax<D>(vt + (long long)key * a.tkv_st, node);
-        if (lane == 0) {
-          const int ke = e4m3_exponent(km), ve = f16_exponent(vm);
-          ctl8->tree_k[group] = ke;
-          ctl8->tree_v[group] = ve;
-          Q8Scales* sc = scales + n_pref;                // (read once the tile's scores are there)
-          reinterpret_cast<float*>(&sc->k)[group] = exp2_int(ke);
-          reinterpret_cast<float*>(&sc->v_log2)[group] = (float)ve;
-          reinterpret_cast<float*>(&sc->v_inv)[group] = exp2_int(-ve);
-        }
-      }
-      named_bar_sync(1, 128);
-      // K: high and low parts, two units of the ring behind those of the prefix
-      int u[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int pos = n_pref + i;
-        u[i] = pos % G::kKUnits;
-        if (ok) ok = wait_c(&ctl8->k_empty[u[i]], ((pos / G::kKUnits) & 1) ^ 1, abort_flag);
-      }
+    if (has_tree && ok) {
+      // the tree's V, to where it will lie and converted there: f16 has bf16's room
+      const __nv_bfloat16* vt = a.Vt + (long long)g * a.tkv_sh + rank * 64;
+      ok = __all_sync(0xffffffffu, wait_c(&ctl->v_empty[vst], vph, abort_flag));
       if (ok) {
-        // PAIR: this CTA's 64 keys, half of the columns a thread
-        const int row = PAIR == 2 ? key & 63 : key, at = PAIR == 2 ? rank * 64 + row : key;
-        const int c0 = PAIR == 2 ? (key >> 6) * (D / 32) : 0;
-        const uint4* src = reinterpret_cast<const uint4*>(kt + (long long)at * a.tkv_st);
-        const float f = exp2_int(-ctl8->tree_k[at >> 5]);
-#pragma unroll 2
-        for (int c = c0; c < c0 + D / 16 / PAIR; ++c)
-          split16(at < p.T ? src[2 * c] : none, at < p.T ? src[2 * c + 1] : none, f,
-                  base + G::k8_off + u[0] * G::kKUnit + code_place<D>(row, c), base + G::k8_off + u[1] * G::kKUnit + code_place<D>(row, c));
-      }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      named_bar_sync(1, 128);
-      if (ok && key == 0) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          arrive_cluster(leader_addr<PAIR>(&ctl8->k_full[u[i]]));
-        }
-      }
-      if (ok) ok = wait_c(&ctl->v_empty[vst], vph, abort_flag);
-      if (ok) {
-        const uint4* src = reinterpret_cast<const uint4*>(vt + (long long)key * a.tkv_st) + rank * 8;
+        constexpr int kLanes = G::kVRow / 8, kStep = 32 / kLanes;          // lanes a node
+        const int c = lane % kLanes;
+        unsigned char* stage = base + G::v_off + vst * G::kVStage;
         const float f = exp2_int(-ctl8->tree_v[group]);
 #pragma unroll 4
-        for (int c = 0; c < G::kVRow / 8; ++c)
-          *reinterpret_cast<uint4*>(base + G::v_off + vst * G::kVStage + f16_place(key, c)) = bf16x8_to_f16x8(key < p.T ? src[c] : none, f);
+        for (int node = group * 32 + lane / kLanes; node < group * 32 + 32; node += kStep)
+          copy_node(stage + f16_place(node, c), vt + (node < p.T ? node * a.tkv_st : 0ll) + 8 * c, node < p.T);
+        copies_wait();
+#pragma unroll 4
+        for (int node = group * 32 + lane / kLanes; node < group * 32 + 32; node += kStep) {
+          uint4* at = reinterpret_cast<uint4*>(stage + f16_place(node, c));
+          *at = bf16x8_to_f16x8(*at, f);
+        }
         publish<PAIR>(&ctl->v_full[vst], lane);
       }
     }
@@ -602,20 +601,90 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
         tma_load<1>(smem_u32(base + G::v_off + ds * 128 * 128), &maps.q, bar, 64 * ds, g * p.G, (rblk * p.RB + rank * 128) / p.G);
     }
     __syncwarp();
-#pragma unroll
-    for (int q = 0; q < kSpxMaxTree / 32; ++q) ctl->parent[lane + 32 * q] = lane + 32 * q < p.T ? a.parent[lane + 32 * q] : -1;
-    __syncwarp();
+    // Masks by doubling: a node's has those of twice as many ancestors after every round.  (Walks up the tree, 32 nodes at a time, took
+    // 130 cycles a level: 16 K for a chain of 60 nodes.)
+    constexpr int kQ = kSpxMaxTree / 32;
+    int up[kQ];                                            // the ancestor that comes next
+    unsigned long long lo[kQ], hi[kQ];
     bool bad = false;
-#pragma unroll 1
-    for (int q = 0; q < kSpxMaxTree / 32; ++q) {
+#pragma unroll
+    for (int q = 0; q < kQ; ++q) {
       const int t = lane + 32 * q;
-      SpxMask128 m = {0ull, 0ull};
-      if (t < p.T) m = spx_walk_up(ctl->parent, p.T, t, bad);
-      ctl->anc[t][0] = m.lo;
-      ctl->anc[t][1] = m.hi;
+      up[q] = t < p.T ? a.parent[t] : -1;
+      if (up[q] < -1 || up[q] >= t) {
+        bad = true;
+        up[q] = -1;
+      }
+      ctl->parent[t] = up[q];
+      ctl->anc[t][0] = lo[q] = t < 64 ? 1ull << (t & 63) : 0ull;
+      ctl->anc[t][1] = hi[q] = t < 64 ? 0ull : 1ull << (t & 63);
+    }
+    __syncwarp();
+#pragma unroll 1
+    while (true) {
+      int most = -1;
+#pragma unroll
+      for (int q = 0; q < kQ; ++q) most = max(most, up[q]);
+      if (!__any_sync(0xffffffffu, most >= 0)) break;      // (ancestors have lower numbers: at most 7 rounds)
+#pragma unroll
+      for (int q = 0; q < kQ; ++q)
+        if (up[q] >= 0) {
+          const int u = up[q];
+          lo[q] |= ctl->anc[u][0];
+          hi[q] |= ctl->anc[u][1];
+          up[q] = ctl->parent[u];
+        }
+      __syncwarp();
+#pragma unroll
+      for (int q = 0; q < kQ; ++q) {
+        const int t = lane + 32 * q;
+        ctl->anc[t][0] = lo[q];
+        ctl->anc[t][1] = hi[q];
+        ctl->parent[t] = up[q];
+      }
+      __syncwarp();
     }
     if (bad && blockIdx.x == 0) spx_raise(a.status, SPECEXT_ERR_BAD_TREE);
     warp_arrive(&ctl->anc_ready, lane);
+    if (has_tree) {
+      // The tree's K is fetched to where it will lie and converted there, row by row: a bf16 row has the bytes of its two parts.  Two tiles
+      // ahead of its turn, by this warp, so that nobody waits for it.  (By the expansion's warps behind the prefix, through
+      // registers, K and V took 9 K to 14 K cycles during which the other workers were done: a load takes 1.4 K cycles while the cache
+      // streams, and few fit in the registers.)
+      const __nv_bfloat16* kt = a.Kt + (long long)g * a.tkv_sh;
+      ok = mbar_wait(&ctl8->tree_go, 0, abort_flag) && mbar_wait(&ctl8->sc_ready, 0, abort_flag);
+      // (this close to the end no barrier of the rings can be a phase behind the one that is waited for)
+      for (int i = 0; i < 2 && ok; ++i)
+        ok = wait_c(&ctl8->k_empty[(n_pref + i) % G::kKUnits], (((n_pref + i) / G::kKUnits) & 1) ^ 1, abort_flag);
+      ok = __all_sync(0xffffffffu, ok);
+      if (ok) {
+        // high and low parts, two units of the ring behind those of the prefix
+        unsigned char *k_hi = base + G::k8_off + n_pref % G::kKUnits * G::kKUnit, *k_lo = base + G::k8_off + (n_pref + 1) % G::kKUnits * G::kKUnit;
+        constexpr int kLanes = D / 16, kStep = 32 / kLanes, kKeys = SPX_TILE_KEYS / PAIR;      // lanes a key; this CTA's keys
+        const int c = lane % kLanes, first = rank * kKeys;
+#pragma unroll 4
+        for (int row = lane / kLanes; row < kKeys; row += kStep) {
+          const bool in = first + row < p.T;
+          const __nv_bfloat16* src = kt + (in ? (first + row) * a.tkv_st : 0ll) + 8 * c;
+          copy_node(k_hi + code_place<D>(row, c), src, in);
+          copy_node(k_lo + code_place<D>(row, c), src + D / 2, in);
+        }
+        copies_wait();
+        __syncwarp();
+        // a lane converts pieces 2 c and 2 c + 1 of a row, which lie in the room of the one part or the other (zeros stay)
+        const unsigned char* raw = c < kLanes / 2 ? k_hi : k_lo;
+        const int c2 = 2 * c % kLanes;
+#pragma unroll 2
+        for (int row0 = 0; row0 < kKeys && first + row0 < p.T; row0 += kStep) {
+          const int row = row0 + lane / kLanes;
+          const uint4 x = *reinterpret_cast<const uint4*>(raw + code_place<D>(row, c2)), y = *reinterpret_cast<const uint4*>(raw + code_place<D>(row, c2 + 1));
+          __syncwarp();
+          split16(x, y, exp2_int(-ctl8->tree_k[(first + row) >> 5]), k_hi + code_place<D>(row, c), k_lo + code_place<D>(row, c));
+        }
+        for (int i = 0; i < 2; ++i) publish<PAIR>(&ctl8->k_full[(n_pref + i) % G::kKUnits], lane);
+      }
+    }
+    if (*abort_flag) ok = false;
   } else {
     // ================================ softmax warps ===========================================
     setmaxnreg_inc<kRegsSoftmaxQ8>();

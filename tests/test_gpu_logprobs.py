@@ -212,3 +212,11 @@ def test_maxima_on_both_sides_of_the_change_of_form(cuda_device):
     wide = (torch.rand((2, V), generator=g, dtype=torch.float64) * 6 - 3).to(dev)
     wide[:, : V // 2] += torch.arange(V // 2, device=dev) * (4.0 / V)
     _check(torch.stack([wide[0] - at, wide[1] + at]).float(), [[0], [V - 1]], 12)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [1, 5, 33])
+def test_many_rows_of_few_words(cuda_device, dtype, V):
+    for offset in (0, 1):
+        x = _logits(1300, V, dtype, cuda_device, 15, V + 1, offset)
+        _check(x, np.zeros((1300, 1), dtype=np.int64), V if V < 33 else 32)
