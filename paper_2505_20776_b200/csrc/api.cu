@@ -347,12 +347,13 @@ int lay_out_rows_q8(AttnPlan* plan) {
 
 // Whether the kernel for few rows takes a call (p: sizes and the plan of the other one).  Up to 16 rows always.  More go there in
 // blocks of 16, each a cluster, which read the same keys again and again: as long as a warp has few steps of 128 keys of its
-// CTA, about 0.68 us each on top of 7, against 1.0 us a tile (0.7 with head_dim 64) on top of 14 (12.5).  us per call, replayed,
-// this kernel / the other (steps, tiles): 60 nodes of 32 query / 8 KV heads 1K 15.8 / 17.2 (9, 1), 2K 20.6 / 17.2 (17, 2); 16 nodes 2K
-// 10.0 / 16.9 (5, 1), 8K 18.0 / 19.0 (17, 4); 10 nodes of 16 / 2 heads 4K 9.6 / 17.8 (4, 1), 16K 15.5 / 22.6 (13, 2); 5 nodes of
-// 32 / 8 16K 21.4 / 23.5 (19, 8), 12 nodes 24.4 / 24.0 (26, 8); 60 nodes of 32 KV heads 1K 16.1 / 17.7 (9, 3), 4K 32.8 / 25.0
-// (33, 9), 20 nodes 8K 30.0 / 31.6 (33, 17); 12 x 64 heads, 60 nodes 1K 10.5 / 14.0 (3, 1), 4K 16.2 / 14.8 (11, 3).  (Blocks of 32
-// rows: 16 nodes 2K 14.0, 10 nodes of 16 / 2 heads 4K 13.0: a step of 32 rows spills and takes more than twice as long.)
+// CTA, about 0.68 us each on top of 7 (6 with head_dim 64), against 0.75 us a tile (0.6) on top of 12.5 (10.4), and 0.08 a worker in the
+// merge.  us per call, replayed, this kernel / the other (steps, tiles, workers): 60 nodes of 32 query / 8 KV heads 1K 13.6 / 15.4
+// (9, 1, 9), 2K 19.0 / 15.5 (17, 2, 9); 16 nodes 2K 9.8 / 14.0 (5, 1, 17), 4K 12.5 / 14.2 (9, 2, 18), 8K 18.0 / 15.1 (17, 4, 18); 10 nodes
+// of 16 / 2 heads 4K 9.6 / 15.3 (4, 1, 33), 16K 15.6 / 20.4 (13, 2, 74); 8 nodes of 32 / 8 8K 14.2 / 14.8 (10, 4, 18), 5 nodes 16K 21.6 /
+// 18.4 (19, 8, 18); 60 nodes of 32 KV heads 1K 14.0 / 15.2 (9, 3, 4), 2K 19.6 / 15.8 (17, 5, 4), 20 nodes 4K 18.4 / 17.8 (17, 9, 4);
+// 12 x 64 heads, 60 nodes 2K 10.1 / 12.1 (6, 2), 4K 13.9 / 12.5 (11, 3), 20 nodes 8K 12.1 / 13.8 (11, 6).  (Blocks of 32 rows: 16 nodes 2K
+// 14.0, 10 nodes of 16 / 2 heads 4K 13.0: a step of 32 rows spills and takes more than twice as long.)
 bool rows_instead(const AttnPlan& p) {
   if (p.want_score) return false;
   if (p.rows <= 16) return true;
@@ -361,7 +362,7 @@ bool rows_instead(const AttnPlan& p) {
   const int size = rows_q8_cluster(problems, (units + 7) / 8);
   if (size == 0) return false;
   const int steps = (units + 8 * size - 1) / (8 * size), tiles = (p.UPP + p.cpp - 1) / p.cpp;
-  return p.D == 64 ? 2 * steps <= 13 + 2 * tiles : 2 * steps <= 20 + 3 * tiles;
+  return p.D == 64 ? 2 * steps <= 13 + 2 * tiles : 2 * steps <= 15 + 2 * tiles + p.cpp / 6;
 }
 
 // The plan of an attention call on the 8-bit cache: every problem has the same whole number of workers.

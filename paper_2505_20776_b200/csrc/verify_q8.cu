@@ -33,6 +33,7 @@ static_assert(256 * (kRegsLaunchQ8 - kRegsOtherQ8) >= 256 * (kRegsSoftmaxQ8 - kR
               "setmaxnreg.inc would wait for registers that are never released");
 constexpr float kHeadroom = 6.0f;              // log2: how far the reference lies below the maximum it was taken from
 constexpr int kMaxUnits = 8;
+constexpr int kTreeAhead = 4;                  // tiles ahead of its turn that the tree's K is begun with
 
 struct Q8Maps {
   CUtensorMap q, k, v;
@@ -50,6 +51,7 @@ struct GeoQ8 {
   static constexpr int kKUnits = kKUnit == 16384 ? 4 : 6, kVUnits = kVUnit == 16384 ? 3 : 6;
   static constexpr uint32_t v_off = 2 * kQ, k8_off = v_off + nv * kVStage, v8_off = k8_off + kKUnits * kKUnit;
   static constexpr int kCtrl = v8_off + kVUnits * kVUnit;
+  static_assert(kTreeAhead + nv <= 2 * kKUnits - 1, "the wait for a unit could take an earlier phase for its own");
   static_assert(nv * kVStage >= 2 * kQ, "the V stages hold the bf16 queries in the beginning");
 };
 
@@ -67,7 +69,7 @@ struct CtrlQ8 {
   uint64_t q_land, q_read;                     // this CTA: the bf16 queries have landed; 8 warps have read them
   uint64_t q_ready;                            // leader: 8 warps per CTA have made their query rows
   uint64_t sc_ready;                           // this CTA: the scales of the run's tiles are in shared memory
-  uint64_t tree_go;                            // this CTA: the expansion is two tiles from the end of the prefix
+  uint64_t tree_go;                            // this CTA: the expansion is kTreeAhead tiles from the end of the prefix
   int tree_k[4], tree_v[4];                    // exponents of the tree's groups of 32 nodes
   uint2 tree_max[4][4];                        // largest magnitudes of K and V of a group, a quarter of the nodes each
   float q_scale[128];
@@ -503,11 +505,11 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
     ok = mbar_wait(&ctl8->q_read, 0, abort_flag) && mbar_wait(&ctl8->sc_ready, 0, abort_flag);        // (they lie where V's stages will be)
     int vc = 0, vst = 0;
     uint32_t vcph = 0, vph = 1;
-    if (n_pref < 2 && key == 0) mbar_arrive(&ctl8->tree_go);
+    if (n_pref < kTreeAhead && key == 0) mbar_arrive(&ctl8->tree_go);
     for (int j = 0; j < n_pref && ok; ++j) {
       ok = mbar_wait(&ctl8->vc_full[vc], vcph, abort_flag) && wait_c(&ctl->v_empty[vst], vph, abort_flag);
       if (!ok) break;
-      if (j == n_pref - 2 && key == 0) mbar_arrive(&ctl8->tree_go);
+      if (j == n_pref - kTreeAhead && key == 0) mbar_arrive(&ctl8->tree_go);
       expand_key<G::kVRow>(base + G::v8_off + vc * G::kVUnit, base + G::v_off + vst * G::kVStage, key);
       publish<PAIR>(&ctl->v_full[vst], lane);
       if (lane == 0) mbar_arrive(&ctl8->vc_empty[vc]);
@@ -647,13 +649,13 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
     if (bad && blockIdx.x == 0) spx_raise(a.status, SPECEXT_ERR_BAD_TREE);
     warp_arrive(&ctl->anc_ready, lane);
     if (has_tree) {
-      // The tree's K is fetched to where it will lie and converted there, row by row: a bf16 row has the bytes of its two parts.  Two tiles
+      // The tree's K is fetched to where it will lie and converted there, row by row: a bf16 row has the bytes of its two parts.  Some tiles
       // ahead of its turn, by this warp, so that nobody waits for it.  (By the expansion's warps behind the prefix, through
       // registers, K and V took 9 K to 14 K cycles during which the other workers were done: a load takes 1.4 K cycles while the cache
       // streams, and few fit in the registers.)
       const __nv_bfloat16* kt = a.Kt + (long long)g * a.tkv_sh;
       ok = mbar_wait(&ctl8->tree_go, 0, abort_flag) && mbar_wait(&ctl8->sc_ready, 0, abort_flag);
-      // (this close to the end no barrier of the rings can be a phase behind the one that is waited for)
+      // (PV of tile n_pref - kTreeAhead - nv is done, so no barrier of the ring can be a phase behind the one that is waited for)
       for (int i = 0; i < 2 && ok; ++i)
         ok = wait_c(&ctl8->k_empty[(n_pref + i) % G::kKUnits], (((n_pref + i) / G::kKUnits) & 1) ^ 1, abort_flag);
       ok = __all_sync(0xffffffffu, ok);
