@@ -506,12 +506,14 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
       reinterpret_cast<float*>(&sc->v_inv)[i & 3] = e8m0_value(vcode == 255u ? 255u : 254u - vcode);
     }
     warp_arrive(&ctl8->sc_ready, lane);
-    ok = mbar_wait(&ctl8->q_read, 0, abort_flag) && mbar_wait(&ctl8->sc_ready, 0, abort_flag);        // (they lie where V's stages will be)
+    // (the queries lie where V's stages will be)
+    ok = __all_sync(0xffffffffu, mbar_wait(&ctl8->q_read, 0, abort_flag) && mbar_wait(&ctl8->sc_ready, 0, abort_flag));
     int vc = 0, vst = 0;
     uint32_t vcph = 0, vph = 1;
     if (n_pref < kTreeAhead && key == 0) mbar_arrive(&ctl8->tree_go);
     for (int j = 0; j < n_pref && ok; ++j) {
-      ok = mbar_wait(&ctl8->vc_full[vc], vcph, abort_flag) && wait_c(&ctl->v_empty[vst], vph, abort_flag);
+      // (all lanes give up, or none: those that go on meet below)
+      ok = __all_sync(0xffffffffu, mbar_wait(&ctl8->vc_full[vc], vcph, abort_flag) && wait_c(&ctl->v_empty[vst], vph, abort_flag));
       if (!ok) break;
       if (j == n_pref - kTreeAhead && key == 0) mbar_arrive(&ctl8->tree_go);
       expand_key<G::kVRow>(base + G::v8_off + vc * G::kVUnit, base + G::v_off + vst * G::kVStage, key);
