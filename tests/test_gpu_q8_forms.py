@@ -123,3 +123,41 @@ def test_workers_that_have_only_tree_keys_behind_a_row(cuda_device, Hq, Hkv, D, 
     hp.check()
     K, V = values(c, L)
     check_attention(t["Q"], K, V, t["K_tree"], t["V_tree"], parent, 32, hp.O, hp.lse, None)
+
+
+@pytest.mark.parametrize("L", [0, 130, 500, 900, 1300, 1900, 2400, 3000, 3500, 4200])
+@pytest.mark.parametrize("Hq,Hkv,D,T", [(32, 32, 128, 33), (64, 16, 128, 40), (36, 36, 64, 70)])
+def test_tree_behind_runs_of_any_length(cuda_device, Hq, Hkv, D, T, L):
+    """Workers of one to nine tiles, so that the tree's comes first, second, .. in its rings (one CTA, pairs, head_dim 64); a chain."""
+    dev = cuda_device
+    c = _filled(Hkv, D, max(L, 1), 64, dev, T + L)
+    c.length = L
+    hp = GuardedHotPath(Hq, Hkv, D, T, 32, 4, max(L, 1), device=dev)
+    t = _tensors(Hq, Hkv, D, T, dev, L)
+    for parent in (random_forest(np.random.default_rng(L), T), np.arange(-1, T - 1, dtype=np.int32)):
+        hp.verify_attn_q8(t, c, torch.from_numpy(parent).to(dev), True)
+        assert hp.read_status() == 0
+        hp.check()
+        K, V = values(c, L)
+        check_attention(t["Q"], K, V, t["K_tree"], t["V_tree"], parent, 32, hp.O, hp.lse, hp.chunk_score(L) if L else None)
+
+
+def test_trees_that_are_none(cuda_device):
+    """A parent behind its node or below -1 is reported, by either kernel; the rows whose path it is not on are as before."""
+    dev, Hq, Hkv, D, T, L = cuda_device, 16, 4, 128, 70, 2100
+    c = _filled(Hkv, D, L, 32, dev, 9)
+    t = _tensors(Hq, Hkv, D, T, dev, 9)
+    good = random_forest(np.random.default_rng(9), T)
+    for scored in (False, True):
+        hp = GuardedHotPath(Hq, Hkv, D, T, 32, 4, L, device=dev)
+        hp.verify_attn_q8(t, c, torch.from_numpy(good).to(dev), scored)
+        assert hp.read_status() == 0
+        O = hp.O.clone()
+        for value in (T + 5, T - 1, -2, 2 ** 31 - 1, -2 ** 31):
+            bad = good.copy()
+            bad[T - 1] = value
+            hp.verify_attn_q8(t, c, torch.from_numpy(bad).to(dev), scored)
+            assert "BAD_TREE" in api.status_bits(hp.read_status())
+            hp.status.zero_()
+            assert torch.equal(hp.O[: T - 1], O[: T - 1])
+            hp.check()
