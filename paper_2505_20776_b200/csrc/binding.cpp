@@ -58,6 +58,11 @@ const at::Tensor& bf16_3d(PyObject* o, const char* what) {
   if (t.scalar_type() != at::kBFloat16 || t.dim() != 3 || t.stride(2) != 1) fail(what);
   return t;
 }
+// K and V of a prefix in bf16, for the calls that take no other (fill_desc makes descriptors for codes as well).
+void bf16_prefix(PyObject* K, PyObject* V) {
+  if (tensor(K).scalar_type() != at::kBFloat16 || tensor(V).scalar_type() != at::kBFloat16)
+    fail("K and V of the prefix must be bf16 (a cache in 8 bits has calls of its own)");
+}
 // A prefix cache: bf16, or the codes of one in 8 bits.
 const at::Tensor& prefix_3d(PyObject* o) {
   const at::Tensor& t = tensor(o);
@@ -210,6 +215,7 @@ PyObject* fill_desc(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // (entry, desc, Q, K_prefix, V_prefix, K_tree, V_tree, parent, O, lse, chunk_score, workspace, device_status)
 PyObject* verify_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 13, [&]() -> PyObject* {
+    bf16_prefix(a[3], a[4]);
     same_strides(a[4], a[3], kStrides);
     same_strides(a[6], a[5], kStrides);
     const Desc d(a[1]);
@@ -230,6 +236,7 @@ PyObject* verify_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* draft_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 13, [&]() -> PyObject* {
     constexpr const char* types = "parent/device_status/n_tokens must be int32 and lse fp32";
+    bf16_prefix(a[3], a[4]);
     same_strides(a[4], a[3], kStrides);
     same_strides(a[7], a[6], kStrides);
     const Desc d(a[1]);

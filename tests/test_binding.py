@@ -48,3 +48,20 @@ def test_select_gather_output_size_does_not_wrap(k, C, layers, heads, dim):
     draft = _fake(1, 1, heads, dim, dtype=torch.bfloat16).expand(layers, 100, heads, dim)
     with pytest.raises(ValueError, match="must be contiguous and hold"):
         _select_gather(_fake(8 * 32, dtype=torch.bfloat16), k, C, draft)
+
+
+@pytest.mark.parametrize("name", ["verify_attn", "draft_attn"])
+@pytest.mark.parametrize("which", ["K", "V", "both"])
+def test_attention_over_a_bf16_prefix_refuses_codes(name, which):
+    """A descriptor may be made for a cache in 8 bits, whose strides are bytes: the calls that read bf16 would read past its end."""
+    T, L, Hq, Hkv, D = 2, 100, 4, 2, 64
+    q, kv, i = _fake(T, Hq, D, dtype=torch.bfloat16), _fake(T, Hkv, D, dtype=torch.bfloat16), _fake(T, dtype=torch.int32)
+    codes, plain = _fake(L, Hkv, D, dtype=torch.float8_e4m3fn), _fake(L, Hkv, D, dtype=torch.bfloat16)
+    K, V = plain if which == "V" else codes, plain if which == "K" else codes
+    d = api.make_attn_desc(q, K, kv, q, L, 32)
+    lse, ws = _fake(Hq, T), _fake(4096, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="must be bf16"):
+        if name == "verify_attn":
+            api.specext_verify_attn(d, q, K, V, kv, kv, i, q, lse, None, ws, i)
+        else:
+            api.specext_draft_attn(d, q, K, V, i, kv, kv, i, q, lse, ws, i)
