@@ -341,7 +341,16 @@ __device__ __forceinline__ bool softmax_tile_q8(const RowCtx& rc, const Q8Scales
     }
     return fmaxf(a, b);
   };
-  const float f0 = mult * ks.x, f1 = mult * ks.y, f2 = mult * ks.z, f3 = mult * ks.w;
+  float f0 = mult * ks.x, f1 = mult * ks.y, f2 = mult * ks.z, f3 = mult * ks.w;
+  if (need_mask) {
+    // A masked score is -inf, and times a factor that fell to zero (a small query on a block of zeros) it would be NaN.  (Scores are
+    // below 2^25: times the least normal number they are still nothing.  A NaN scale stays.)
+    auto positive = [](float f) { return f < 1.17549435e-38f ? 1.17549435e-38f : f; };
+    f0 = positive(f0);
+    f1 = positive(f1);
+    f2 = positive(f2);
+    f3 = positive(f3);
+  }
   const float m_tile = fmaxf(fmaxf(fmaf(max_group(s0), f0, ev.x), fmaf(max_group(s1), f1, ev.y)),
                              fmaxf(fmaf(max_group(s2), f2, ev.z), fmaf(max_group(s3), f3, ev.w))) - kHeadroom;
 
