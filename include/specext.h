@@ -176,7 +176,8 @@ int specext_verify_attn_q8(const specext_attn_desc* desc, const specext_q8_desc*
  *   logprob : fp32 [n_rows][n_given];  entropy, lse : fp32 [n_rows];
  *   top_ids : int32, top_logprob : fp32, [n_rows][n_best], 0 <= n_best <= min(32, vocab).
  * A row without a finite logit (all -inf) has lse = -inf, log probabilities -inf and entropy 0; a row
- * with a NaN or +inf has NaN everywhere and top_ids -1.  Sums are fp32; the logits are read once.
+ * with a NaN or +inf has NaN everywhere and top_ids -1.  Sums are fp32; no log probability is above 0 and no
+ * entropy below, and where one word has nearly all the probability both are as exact, relative to themselves, as elsewhere.
  */
 int specext_token_logprobs(const void* logits, int32_t logits_fp32, int32_t n_rows, int32_t vocab,
                            int64_t stride_row, float temperature, const int32_t* tokens,

@@ -9,7 +9,7 @@ cudaError_t spx_launch_quantize(const void* K, const void* V, int n_kv_heads, in
                                 const int32_t* rows, int n_src, int n, int start, void* Kc, void* Vc, long long c_sl,
                                 long long c_sh, void* Ks, void* Vs, long long s_sb, long long s_sh, int log_block,
                                 int32_t* status, cudaStream_t st);
-cudaError_t spx_launch_logprobs(const void* logits, bool f32, int rows, int V, long long stride, float inv_temperature,
+cudaError_t spx_launch_logprobs(const void* logits, bool f32, int rows, int V, long long stride, float temperature,
                                 const int32_t* tokens, int given, int best, float* logprob, float* entropy, float* lse,
                                 int32_t* top_ids, float* top_logprob, int n_sm, int32_t* status, cudaStream_t st);
 cudaError_t spx_launch_select(const float* score_row, int NC, int L, int C, int k, int n_sink, int n_recent,
@@ -598,7 +598,7 @@ int specext_token_logprobs(const void* logits, int32_t logits_fp32, int32_t n_ro
                           reinterpret_cast<uintptr_t>(entropy) | reinterpret_cast<uintptr_t>(lse) |
                           reinterpret_cast<uintptr_t>(top_ids) | reinterpret_cast<uintptr_t>(top_logprob);
   if ((words & 3u) != 0 || (reinterpret_cast<uintptr_t>(logits) & (logits_fp32 ? 3u : 1u)) != 0) return SPECEXT_ERR_INVALID_ARG;
-  const cudaError_t e = spx_launch_logprobs(logits, logits_fp32 != 0, n_rows, vocab, stride_row, 1.f / temperature, tokens, n_given,
+  const cudaError_t e = spx_launch_logprobs(logits, logits_fp32 != 0, n_rows, vocab, stride_row, temperature, tokens, n_given,
                                             n_best, logprob, entropy, lse, top_ids, top_logprob, sm_count(), device_status,
                                             static_cast<cudaStream_t>(cuda_stream));
   g_launches.fetch_add(1);

@@ -1,8 +1,16 @@
 // Log probabilities under rows of logits: of given tokens, of the k best words, and the row's entropy.  With x = logits /
 // temperature, m its maximum, Z = sum e^(x - m) and E = sum e^(x - m) (x - m):
 //   lse = m + log Z,  log p(w) = (x_w - m) - log Z,  entropy = -sum p log p = log Z - E / Z.
-// One pass over the logits with running m, Z and E in fp32 (32 words share one rescaling); a row is split over the CTAs of a
-// cluster where rows are few, and joined in the first CTA's shared memory.
+// One pass over the logits with running m, Z and E in fp32 (a thread's 16 or 32 words of a turn share one rescaling); a row is
+// split over the CTAs of a cluster where rows are few, and joined in the first CTA's shared memory.
+//
+// Where one word has nearly all of the probability, what is left to the others decides the results: with r = Z - 1, the sum of all
+// words but the best, log Z = log1p(r), the best word's log probability is -log1p(r), the entropy log1p(r) - E / (1 + r), all terms of
+// one sign, so that nothing cancels and no log probability is above 0, no entropy below.  So partial results are joined without their
+// best word (1 and 0 to Z and E, exactly).  Only the thread that has the row's best word gets its part of r by a difference,
+// Z - 1, which is off by some 2^-22; where r is below 1/2 the CTA sums that thread's words again without the best one.  (us per call,
+// replayed, before / with it: one row of 32000 bf16 5.3 / 5.6, 60 of 128256 10.6 / 11.1, 2047 of 32000 fp32 53.0 / 53.9; the sum out of line,
+// in a function of its own, 55.6 for the last.)
 //
 // The best words are found without sorting: a word's key is (logit, lower index first).  Every thread knows its own best key
 // after the pass (up to its place in a vector); the k-th best of the warps' j best thread keys (j times the number of warps >= k)
@@ -25,7 +33,7 @@ namespace {
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kNextRow = 32768;
 constexpr int kMaxBest = 32, kMaxSlices = 8, kList = 512;
-constexpr float kLn2 = 0.693147180559945309417f, kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.693147180559945309417f;
 typedef unsigned long long Key;                 // 0: none
 
 struct LogprobArgs {
@@ -35,7 +43,7 @@ struct LogprobArgs {
   int32_t *top_ids, *status;
   long long stride;
   int V, given, best, slices, resident;
-  float inv_temperature;
+  float inv_temperature, c;                     // c = log2 e / temperature, rounded once
 };
 
 __device__ __forceinline__ uint32_t ordered(float x) {         // no NaN; -0 counts as 0
@@ -140,7 +148,7 @@ __device__ __forceinline__ Scale scale_of(float c) {
   const bool usual = c > 1e-20f && c < 1e6f;
   return {c, usual ? kLarge / c : 0.f, usual ? kSlack / c : 0.f};
 }
-// `s` relative to a maximum m >= s.m.
+// `s` relative to a new reference m >= s.m (of one thread, in the pass).
 __device__ __forceinline__ Stat at_maximum(Stat s, float m, const Scale& sc) {
   const bool plain = fabsf(m) < sc.plain, was = fabsf(s.m) < sc.plain;
   const float to = __fmul_rn(m, sc.c), from = __fmul_rn(s.m, sc.c);
@@ -150,26 +158,68 @@ __device__ __forceinline__ Stat at_maximum(Stat s, float m, const Scale& sc) {
   if (s.z == 0.f) return {m, 0.f, 0.f};
   return {m, s.z * f, f == 0.f ? 0.f : f * fmaf(d, s.z, s.e)};
 }
-// The joint statistics of stats[0 .. n), n <= 8, by every warp for itself: a lane has one of them.
-__device__ __forceinline__ Stat join(const Stat* stats, int n, const Scale& sc) {
+// ... and relative to the logit m itself: t is (x - m) c from here on, without the rounding of m c.
+__device__ __forceinline__ Stat relative_to(Stat s, float m, const Scale& sc) {
+  const float d = fabsf(s.m) < sc.plain ? -fmaf(m, sc.c, -__fmul_rn(s.m, sc.c)) : (s.m - m) * sc.c;
+  const float f = ex2_approx(d);
+  if (s.z == 0.f) return {m, 0.f, 0.f};
+  return {m, s.z * f, f == 0.f ? 0.f : f * fmaf(d, s.z, s.e)};
+}
+// (x - m) c, for any words x <= m.
+struct Difference {
+  float m, c, to, off;                          // m c, and what it was rounded by
+  bool plain;
+  __device__ __forceinline__ float operator()(float x) const { return plain ? fmaf(x, c, -to) - off : (x - m) * c; }
+};
+__device__ __forceinline__ Difference difference_to(float m, const Scale& sc) {
+  const float to = __fmul_rn(m, sc.c);
+  return {m, sc.c, to, fmaf(m, sc.c, -to), fabsf(m) < sc.plain};
+}
+// What the thread with a warp's best word has beside that word, and which thread it is (-1: none but -inf and NaN).
+struct Own {
+  float z, e;
+  int tid;
+};
+// The joint statistics of stats[0 .. n), n <= 8, by every warp for itself: a lane has one of them.  z and e are without the best
+// word, of what goes in and of what comes out; of stats with parts of their own, `own` is that of the best, which the result leaves out.
+template <bool OWN>
+__device__ __forceinline__ Stat join(const Stat* stats, int n, const Scale& sc, const Own* owns, Own* own) {
   const int i = threadIdx.x & 7;
   Stat s = {-INFINITY, 0.f, 0.f};
-  if (i < n) s = stats[i];
+  Own mine = {0.f, 0.f, -1};
+  if (i < n) {
+    s = stats[i];
+    if (OWN) mine = owns[i];
+  }
   float m = s.m;
 #pragma unroll
   for (int o = 1; o < 8; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  s = at_maximum(s, m, sc);
+  const bool some = s.m > -INFINITY;
+  const int best = __ffs(__ballot_sync(0xffffffffu, some && s.m == m)) - 1;
+  if (i != best) {
+    s.z += mine.z;
+    s.e += mine.e;
+    if (some) {
+      const float d = difference_to(m, sc)(s.m), f = ex2_approx(d), z = s.z + 1.f;
+      s.z = z * f;
+      s.e = f == 0.f ? 0.f : f * fmaf(d, z, s.e);
+    }
+  }
 #pragma unroll
   for (int o = 1; o < 8; o <<= 1) {
     s.z += __shfl_xor_sync(0xffffffffu, s.z, o);
     s.e += __shfl_xor_sync(0xffffffffu, s.e, o);
   }
+  s.m = m;
+  if (OWN) *own = best >= 0 ? owns[best] : Own{0.f, 0.f, -1};
   return s;
 }
 static_assert(kWarps <= 8 && kMaxSlices <= 8, "join has 8 lanes");
 
 struct Shared {
   Stat warp_stat[kWarps];
+  Own warp_own[kWarps];
+  float2 again_sum;                             // z and e of the best word's thread, summed again
   Key bounds[kWarps * kMaxBest];                // the warps' best thread keys
   Key list[kList];
   Key top[kMaxBest];
@@ -223,8 +273,10 @@ __device__ __forceinline__ void each_key(const Row<F32>& row, int v, Use&& use) 
 
 // The `best` best keys of the words in vectors [lo, hi) to sh.top, in order (zeros where there are no more words).  `mine`: no word
 // of the thread has a better key; `full` warps had a vector for every thread, and their best thread keys are in sh.bounds.
-template <bool F32>
-__device__ __forceinline__ void best_words(Shared& sh, const Row<F32>& row, int lo, int hi, int best, Key mine, int turn, int n_turn, Key rest, int full) {
+// `meanwhile`: done beside the second look, which the first warps have.
+template <bool F32, class Meanwhile>
+__device__ __forceinline__ void best_words(Shared& sh, const Row<F32>& row, int lo, int hi, int best, Key mine, int turn, int n_turn, Key rest, int full,
+                                           Meanwhile&& meanwhile) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   // The bound: of the warps' best thread keys (j of each, at least k in all) the k-th best; or the lowest, where they are too many
   // for a warp to look at.
@@ -255,6 +307,7 @@ __device__ __forceinline__ void best_words(Shared& sh, const Row<F32>& row, int 
         }
       });
   }
+  meanwhile();
   __syncthreads();
   const int n = sh.n_list;
   if (n <= kList) {
@@ -311,7 +364,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(const __grid_const
   const Row<F32> row(a, r);
   const int per = (row.n_vec + n_slices - 1) / n_slices;
   const int lo = min(row.n_vec, rank * per), hi = min(row.n_vec, lo + per);
-  const Scale sc = scale_of(a.inv_temperature * kLog2e);
+  const Scale sc = scale_of(a.c);
   pdl_wait();
   // the first given tokens' logits, ahead of the pass
   int token = -1;
@@ -409,7 +462,11 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(const __grid_const
   float m = top_value;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  s = at_maximum(s, m, sc);
+  s = relative_to(s, m, sc);
+  const int best_lane = __ffs(__ballot_sync(0xffffffffu, top_value == m && m > -INFINITY)) - 1;
+  if (lane == best_lane) sh.warp_own[warp] = {s.z - 1.f, s.e, tid};
+  if (best_lane < 0 && lane == 0) sh.warp_own[warp] = {0.f, 0.f, -1};
+  if (lane == best_lane) s.z = s.e = 0.f;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     s.z += __shfl_xor_sync(0xffffffffu, s.z, o);
@@ -433,11 +490,52 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(const __grid_const
     }
   }
   __syncthreads();
-  s = join(sh.warp_stat, kWarps, sc);
+  Own own;
+  s = join<true>(sh.warp_stat, kWarps, sc, sh.warp_own, &own);
+  // The best word is nearly all there is: its thread's other words (an equal word would weigh 1, so none is there), by the last warp.
+  const bool again = own.tid >= 0 && s.z + own.z < 0.5f;
+  const bool summing = again && warp == kWarps - 1;
+  int v_again = lo + own.tid + lane * kThreads;
+  uint4 raw_again = none<F32>();
+  if (summing && v_again < hi) raw_again = load_vec(row, v_again);            // (on its way while the best words are looked for)
+  auto sum_again = [&]() {
+    if (!summing) return;
+    const Difference diff = difference_to(s.m, sc);
+    float z = 0.f, e = 0.f;
+#pragma unroll 1
+    while (true) {
+      float x[W];
+      unpack<F32>(raw_again, x);
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        const float t = diff(x[j]), q = x[j] == s.m ? 0.f : ex2_approx(t);
+        z += q;
+        e = fmaf(q, fmaxf(t, -1e30f), e);
+      }
+      v_again += 32 * kThreads;
+      if (v_again >= hi) break;
+      raw_again = load_vec(row, v_again);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      z += __shfl_xor_sync(0xffffffffu, z, o);
+      e += __shfl_xor_sync(0xffffffffu, e, o);
+    }
+    if (lane == 0) sh.again_sum = make_float2(z, e);
+  };
   if (a.best > 0) {
     const int turn = lo + tid + (top_v - lo - tid) / kTurn * kTurn;
-    best_words(sh, row, lo, hi, a.best, mine, turn, kTurn, make_key(other, 0), full);
+    best_words(sh, row, lo, hi, a.best, mine, turn, kTurn, make_key(other, 0), full, sum_again);
+  } else {
+    sum_again();
+    __syncthreads();
   }
+  if (again) {
+    own.z = sh.again_sum.x;
+    own.e = sh.again_sum.y;
+  }
+  s.z += own.z;
+  s.e += own.e;
 
   const Key* keys = sh.top;
   int n_keys = a.best;
@@ -462,21 +560,19 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(const __grid_const
       settle();
       return;
     }
-    s = join(sh.stat, n_slices, sc);
+    s = join<false>(sh.stat, n_slices, sc, nullptr, nullptr);
     keys = sh.keys;
     n_keys = n_slices * a.best;
   }
 
-  // log(z) of a row without a finite logit is -inf: all its log probabilities are, and its entropy is 0
-  const bool empty = s.z == 0.f;
-  // log Z relative to m itself: what m c was rounded by is put right
-  const float log2_z = log2f(s.z), off = fabsf(s.m) < sc.plain ? fmaf(s.m, sc.c, -__fmul_rn(s.m, sc.c)) : 0.f;
-  const float log_z = (log2_z - off) * kLn2, lse = empty ? -INFINITY : fmaf(s.m, a.inv_temperature, log_z);
+  // a row without a finite logit: all its log probabilities are -inf, and its entropy is 0
+  const bool empty = s.m == -INFINITY && s.z == 0.f;
+  const float log_z = log1pf(s.z), lse = empty ? -INFINITY : fmaf(s.m, a.inv_temperature, log_z);
   // (the difference to the maximum first: x - lse would lose log Z where the maximum is huge, as in a row of the type's lowest value)
   auto log_p = [&](float raw) { return empty ? -INFINITY : fmaf(raw - s.m, a.inv_temperature, -log_z); };
   if (tid == 0) {
     a.lse[r] = lse;
-    a.entropy[r] = empty ? 0.f : (log2_z - s.e / s.z) * kLn2;
+    a.entropy[r] = empty ? 0.f : log_z - s.e / (1.f + s.z) * kLn2;
   }
   for (int i = tid; i < a.given; i += kThreads) {
     const long long at = (long long)r * a.given + i;
@@ -523,13 +619,15 @@ cudaError_t launch(const LogprobArgs& a, int rows, cudaStream_t st) {
 
 }  // namespace
 
-cudaError_t spx_launch_logprobs(const void* logits, bool f32, int rows, int V, long long stride, float inv_temperature,
+cudaError_t spx_launch_logprobs(const void* logits, bool f32, int rows, int V, long long stride, float temperature,
                                 const int32_t* tokens, int given, int best, float* logprob, float* entropy, float* lse,
                                 int32_t* top_ids, float* top_logprob, int n_sm, int32_t* status, cudaStream_t st) {
   LogprobArgs a;
   a.logits = logits; a.tokens = tokens;
   a.logprob = logprob; a.entropy = entropy; a.lse = lse; a.top_ids = top_ids; a.top_logprob = top_logprob; a.status = status;
-  a.stride = stride; a.V = V; a.given = given; a.best = best; a.inv_temperature = inv_temperature;
+  a.stride = stride; a.V = V; a.given = given; a.best = best;
+  a.inv_temperature = 1.f / temperature;
+  a.c = (float)(1.4426950408889634074 / (double)temperature);
   // CTAs per row: as many as are resident at once (four per SM), as long as a thread has two vectors and more.  us per call, 1 / 2 /
   // 4 / 8: one row of 32000 bf16 6.6 / 5.8 / 5.3 / 5.4, 16 of 128256 27 / 15.7 / 10.4 / 8.7, 60 of 128256 28 / 16.8 / 13.5 / 10.8, 200 of
   // 32000 fp32 12.6 / 11.2 / 15.3 / 22.9
