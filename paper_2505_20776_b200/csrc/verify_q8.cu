@@ -765,8 +765,10 @@ verify_q8_kernel(const __grid_constant__ Q8Args args, const __grid_constant__ Q8
       const bool is_tree = tile == p.TPH;
       const int nkeys = is_tree ? p.T : min(SPX_TILE_KEYS, p.L - tile * SPX_TILE_KEYS);
       if (!known || is_tree) {
-        // (the scores are there, so the query rows and the tree's scales are)
-        ok = mbar_wait(&ctl->s_full[rc.w], (j / kWG) & 1, abort_flag) && mbar_wait(&ctl8->sc_ready, 0, abort_flag);
+        // (the scores are there, so these have long been; but the row's factor was written by another warp of this CTA, and the way
+        // from there to here by q_ready, the leader's products and s_full goes through another CTA and orders no plain stores)
+        ok = mbar_wait(&ctl->s_full[rc.w], (j / kWG) & 1, abort_flag) && mbar_wait(&ctl8->sc_ready, 0, abort_flag) &&
+             mbar_wait(&ctl8->q_read, 0, abort_flag);
         if (ok && is_tree) ok = mbar_wait(&ctl->anc_ready, 0, abort_flag);
         if (!ok) break;
         mult = p.scale2 * ctl8->q_scale[rc.row_t];

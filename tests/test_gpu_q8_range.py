@@ -49,3 +49,20 @@ def test_a_tree_of_tiny_queries_and_keys(cuda_device, Hq, Hkv, D, T, scored, dow
     t["K_tree"] *= 2.0 ** -down
     hp = GuardedHotPath(Hq, Hkv, D, T, 32, 4, L, device=dev)
     _check(hp, t, c, random_forest(np.random.default_rng(down), T), scored)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,T,scored", [(8, 4, 128, 17, True), (32, 8, 128, 60, True), (32, 8, 128, 40, False), (64, 8, 128, 128, False)])
+def test_every_row_has_a_size_of_its_own(cuda_device, Hq, Hkv, D, T, scored):
+    """Query rows each at another power of two, in another order every time: a row's factor is the one its own warp found, in both
+    CTAs of a pair, whatever the call before left in its place."""
+    dev, L = cuda_device, 3000
+    g = torch.Generator().manual_seed(T)
+    c = _cache(dev, Hkv, D, *(torch.randn((L, Hkv, D), generator=g) for _ in range(2)))
+    hp = GuardedHotPath(Hq, Hkv, D, T, 32, 4, L, device=dev)
+    parent = random_forest(np.random.default_rng(T), T)
+    t = _tensors(Hq, Hkv, D, T, dev, T)
+    plain = t["Q"]
+    for turn in range(3):
+        size = torch.exp2(torch.randint(-12, 3, (T, Hq, 1), generator=g).float()).to(dev)
+        t["Q"] = (plain.float() * size).to(torch.bfloat16)
+        _check(hp, t, c, parent, scored)
