@@ -151,3 +151,30 @@ def test_cache_refusals():
             c.append(K[:n], K[:n], start=start)
     with pytest.raises(ValueError, match="CUDA"):                    # there is no CPU path
         c.append(K[:1], K[:1])
+
+
+@pytest.mark.parametrize("rows,text", [
+    (_fake(4, dtype=torch.int64), "rows must be"), (_fake(4, 1, dtype=torch.int32), "rows must be"),
+    (_fake(8, dtype=torch.int32)[::2], "rows must be"), (_fake(101, dtype=torch.int32), "does not hold"),
+])
+def test_what_the_binding_says_of_rows(rows, text):
+    """By its own message (a call that passes every check ends with another error, where the stream is asked for)."""
+    with pytest.raises(ValueError, match=text):
+        _call_quantize(rows=rows)
+
+
+@pytest.mark.parametrize("kw,text", [
+    (dict(tokens=_fake(3, 2, dtype=torch.int64), lp=_fake(3, 2, dtype=torch.float32)), "tokens must be"),
+    (dict(tokens=_fake(2, 2, dtype=torch.int32), lp=_fake(2, 2, dtype=torch.float32)), "tokens must be"),
+    (dict(tokens=_fake(3, 2, dtype=torch.int32), lp=_fake(3, 3, dtype=torch.float32)), "tokens must be"),
+    (dict(tokens=_fake(3, 2, dtype=torch.int32), lp=_fake(3, 2)), "tokens must be"),
+    (dict(tokens=_fake(3, dtype=torch.int32), lp=_fake(3, dtype=torch.float32)), "tokens must be"),
+    (dict(tokens=_fake(2, 3, dtype=torch.int32).t(), lp=_fake(3, 2, dtype=torch.float32)), "tokens must be"),
+    (dict(ids=_fake(3, 2, dtype=torch.int32), top=_fake(3, 1, dtype=torch.float32)), "top_ids must be"),
+    (dict(ids=_fake(3, 2, dtype=torch.int64), top=_fake(3, 2, dtype=torch.float32)), "top_ids must be"),
+    (dict(ent=_fake(2, dtype=torch.float32)), "entropy and lse"), (dict(ent=_fake(3)), "entropy and lse"),
+    (dict(ids=_fake(3, 2, dtype=torch.int32)), "go together"),
+])
+def test_what_the_binding_says_of_tables(kw, text):
+    with pytest.raises(ValueError, match=text):
+        _call_logprobs(**kw)
