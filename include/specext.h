@@ -172,7 +172,7 @@ int specext_verify_attn_q8(const specext_attn_desc* desc, const specext_q8_desc*
  *   logits  : bf16, or fp32 when logits_fp32 != 0, [n_rows][vocab] with row stride stride_row >= vocab (any), any
  *             alignment of its type; -inf (a masked word) is allowed.  vocab <= 2^30.
  *   tokens  : int32 [n_rows][n_given]; -1 is "no token" and gets -inf; others outside [0, vocab) get -inf and are
- *             reported as INVALID_ARG in *device_status.  n_given may be 0.
+ *             reported as INVALID_ARG in *device_status.  n_given may be 0; n_given <= 2^30.
  *   logprob : fp32 [n_rows][n_given];  entropy, lse : fp32 [n_rows];
  *   top_ids : int32, top_logprob : fp32, [n_rows][n_best], 0 <= n_best <= min(32, vocab).
  * A row without a finite logit (all -inf) has lse = -inf, log probabilities -inf and entropy 0; a row

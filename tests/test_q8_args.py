@@ -178,3 +178,10 @@ def test_what_the_binding_says_of_rows(rows, text):
 def test_what_the_binding_says_of_tables(kw, text):
     with pytest.raises(ValueError, match=text):
         _call_logprobs(**kw)
+
+
+@pytest.mark.parametrize("given", [(1 << 30) + 1, (1 << 31) - 1])
+def test_more_given_tokens_than_a_loop_of_int32_counts(lib, given):
+    """A loop over them in steps of a thread block would pass 2^31 and go on behind 0."""
+    assert _logprobs(lib, given=given) == UNSUPPORTED
+    assert _logprobs(lib, given=given, rows=0) == UNSUPPORTED
