@@ -169,6 +169,7 @@ int specext_verify_attn_q8(const specext_attn_desc* desc, const specext_q8_desc*
  *   lse = log sum_w e^(x_w),  logprob[i] = x[tokens[i]] - lse,  entropy = -sum_w p_w log p_w (nats),
  *   top_ids / top_logprob: the n_best largest logits in descending order, equal ones by the lower index.
  *
+ *   temperature : above 0 and finite, and so is log2(e) / temperature (INVALID_ARG otherwise).
  *   logits  : bf16, or fp32 when logits_fp32 != 0, [n_rows][vocab] with row stride stride_row >= vocab (any), any
  *             alignment of its type; -inf (a masked word) is allowed.  vocab <= 2^30.
  *   tokens  : int32 [n_rows][n_given]; -1 is "no token" and gets -inf; others outside [0, vocab) get -inf and are

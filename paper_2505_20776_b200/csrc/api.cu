@@ -590,7 +590,9 @@ int specext_token_logprobs(const void* logits, int32_t logits_fp32, int32_t n_ro
                            void* cuda_stream) {
   if (n_rows < 0 || vocab < 1 || n_given < 0 || n_best < 0 || n_best > vocab || stride_row < vocab) return SPECEXT_ERR_INVALID_ARG;
   if (vocab > (1 << 30) || n_given > (1 << 30) || n_best > 32 || (long long)n_rows > (1ll << 27)) return SPECEXT_ERR_UNSUPPORTED;
-  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.f / temperature)) return SPECEXT_ERR_INVALID_ARG;
+  // (log2 e / temperature is what the kernel multiplies with)
+  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite((float)(1.4426950408889634074 / (double)temperature)))
+    return SPECEXT_ERR_INVALID_ARG;
   if (n_rows == 0) return SPECEXT_OK;
   if (!logits || !entropy || !lse || (n_given > 0 && (!tokens || !logprob)) || (n_best > 0 && (!top_ids || !top_logprob)))
     return SPECEXT_ERR_INVALID_ARG;

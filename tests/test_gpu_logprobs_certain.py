@@ -122,3 +122,24 @@ def test_rows_that_more_than_one_word_rules(cuda_device):
     x[torch.arange(48), 300 + 70 * torch.arange(48)] = 10.0 - 0.0625 * torch.arange(1, 49)
     _check(x.to(dev), 1.0)
     _check(x.to(torch.bfloat16).to(dev), 1.0, 2)
+
+
+def test_temperatures_at_the_ends(cuda_device):
+    """As cold as a float allows (the best word is certain) and as hot (all words that are not masked are alike)."""
+    dev, V = cuda_device, 9001
+    x = _rows(4, V, torch.float32, dev, 9)
+    x[3, ::2] = float("-inf")
+    hp = GuardedHotPath(1, 1, 64, 1, 32, 1, 1, device=dev)
+    best = x.argmax(1, keepdim=True).to(torch.int32)
+    for T in (4.3e-39, 1e-38, 1e-30, 1e-10):
+        lp, ent, lse, ids, top = hp.token_logprobs(x, best, 2, T)
+        assert hp.read_status() == 0
+        assert (lp == 0).all() and (ent == 0).all() and (ids[:, :1] == best).all() and (top[:, 0] == 0).all() and (top[:, 1] < 0).all()
+        assert not lse.isnan().any()
+    n = torch.tensor([V, V, V, V // 2], dtype=torch.float64)
+    for T in (1e20, 1e30, 3e38):
+        lp, ent, lse, ids, top = hp.token_logprobs(x, best, 2, T)
+        assert hp.read_status() == 0
+        for got in (ent, lse, -lp[:, 0], -top[:, 1]):
+            np.testing.assert_allclose(f64(got), n.log().numpy(), rtol=1e-6)
+    hp.check()

@@ -185,3 +185,10 @@ def test_more_given_tokens_than_a_loop_of_int32_counts(lib, given):
     """A loop over them in steps of a thread block would pass 2^31 and go on behind 0."""
     assert _logprobs(lib, given=given) == UNSUPPORTED
     assert _logprobs(lib, given=given, rows=0) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("T", [3e-39, 4e-39])
+def test_temperatures_whose_factor_is_no_number(lib, T):
+    """1 / T is a finite number there, log2(e) / T is not: 0 times it made every row NaN."""
+    assert _logprobs(lib, T=T) == INVALID
+    assert _logprobs(lib, T=T, rows=0) == INVALID and _logprobs(lib, T=4.3e-39, rows=0) == OK
