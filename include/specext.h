@@ -96,6 +96,7 @@ size_t specext_verify_attn_workspace(const specext_attn_desc* desc);
  *   workspace   : scratch of at least specext_verify_attn_workspace(desc) bytes.
  * Arithmetic: bf16 products accumulated in fp32; probabilities are rounded to bf16 for the
  * P*V product; chunk sums and the normaliser are accumulated in fp32 from unrounded exponentials.
+ * V_tree must be finite: a NaN or infinity there, unlike one in K_tree, also reaches the nodes of its head that do not see its node.
  */
 int specext_verify_attn(const specext_attn_desc* desc, const void* Q, const void* K_prefix,
                         const void* V_prefix, const void* K_tree, const void* V_tree,
@@ -146,8 +147,8 @@ int specext_quantize_kv(const void* K, const void* V, int32_t n_src, int32_t n_k
  * to a block with a finite scale, are NaN.
  * Arithmetic: the result is that of attention on the values the cache stands for (magnitudes up to 2^100).  Products
  * of queries and codes are exact but for query and tree values that lie far below the largest of their row or of
- * their 32 nodes (those 2^-10 of it and less are kept to 2^-18 of it, for up to 16 rows per KV head to 2^-39) and are
- * accumulated in fp32; probabilities, times the V scale, are rounded to f16 for the product with V (11 bits;
+ * their 32 nodes (those below 2^-9 of it are kept to 2^-17 of it; to 2^-39 in calls without chunk scores of up to 16 rows,
+ * query heads times nodes, per KV head) and are accumulated in fp32; probabilities, times the V scale, are rounded to f16 for the product with V (11 bits;
  * 2^-30 and less of a row's largest counts as zero); chunk sums and the normaliser are accumulated in fp32 from
  * unrounded exponentials.  V's scale is part of the exponent: where the V scales of a head's blocks (2^-100 for a block of
  * zeros) lie 2^d apart, d > 100, weights of 2^(d-132) of the largest and less are lost in the blocks of the lowest (2^-30 and

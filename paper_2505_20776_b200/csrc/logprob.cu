@@ -336,8 +336,9 @@ __device__ __forceinline__ void best_words(Shared& sh, const Row<F32>& row, int 
 }
 
 // AHEAD: more rows than CTAs at once, so that reading is what counts: two turns ahead go to L2, and the next row's beginning while this
-// one's words are put in order.  us per call with / without: 2047 rows of 32000 fp32 53.3 / 58.6, bf16 42.5 / 45.6, 1500 of 128256 bf16
-// 86 / 93; 200 of 32000 fp32 13.2 / 11.2, 500 of 128256 bf16 38 / 36.9.  (128 threads and twice the CTAs: 56.9 and 39.4 of the first and last.)
+// one's words are put in order.  us per call, replayed, with / without: 2047 rows of 32000 fp32 52.4 / 57.4, bf16 40.2 / 44.7, 1500 of
+// 128256 bf16 84.5 / 94; before rows that one word dominates were summed again, 200 of 32000 fp32 13.2 / 11.2, 500 of 128256 bf16 38 / 36.9 (128
+// threads and twice the CTAs: 56.9 and 39.4 where it was 53.3 and 38).
 template <bool F32, bool AHEAD>
 __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(const __grid_constant__ LogprobArgs a) {
   constexpr int W = Row<F32>::kWords;
@@ -629,8 +630,8 @@ cudaError_t spx_launch_logprobs(const void* logits, bool f32, int rows, int V, l
   a.inv_temperature = 1.f / temperature;
   a.c = (float)(1.4426950408889634074 / (double)temperature);
   // CTAs per row: as many as are resident at once (four per SM), as long as a thread has two vectors and more.  us per call, 1 / 2 /
-  // 4 / 8: one row of 32000 bf16 6.6 / 5.8 / 5.3 / 5.4, 16 of 128256 27 / 15.7 / 10.4 / 8.7, 60 of 128256 28 / 16.8 / 13.5 / 10.8, 200 of
-  // 32000 fp32 12.6 / 11.2 / 15.3 / 22.9
+  // 4 / 8, replayed: one row of 32000 bf16 6.9 / 6.1 / 5.6 / 5.5 (at most 4 by this rule), 16 of 128256 27.2 / 16.0 / 10.6 / 9.0, 60 of
+  // 128256 27.9 / 16.8 / 13.9 / 11.2, 200 of 32000 fp32 12.3 / 11.0 (2 by this rule; 4 and 8 were 15.3 and 22.9)
   const int words = f32 ? 4 : 8;
   int slices = 1;
   while (slices < kMaxSlices && 2ll * rows * slices <= 4ll * n_sm && V / words >= 2 * slices * 2 * kThreads) slices *= 2;

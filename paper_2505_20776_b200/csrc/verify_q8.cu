@@ -4,8 +4,9 @@
 //
 // S = Q K^T is a product of e4m3 by e4m3, twice: a bf16 value has 8 significant bits and is the sum of two e4m3 values of 4, so
 // with the query row taken to [2^7, 2^8) by a power of two its high and low parts, multiplied with the codes as they lie in
-// memory, give S as exactly as bf16 products would (elements 2^-10 of the row's largest and less are kept to 2^-18 of it), in the
-// time of the bf16 products and without touching K.  The tree's bf16 keys are two such tiles, high parts and low parts.
+// memory, give S as exactly as bf16 products would, in the time of the bf16 products and without touching K.  (e4m3's smallest step is
+// 2^-9: elements below 2^-9 of the row's largest are kept to half of it, 2^-17 of the largest.)  The tree's bf16 keys are two such tiles, high parts
+// and low parts, with a power of two per 32 nodes.
 // For O += P V the codes of V become f16 (every e4m3 value is one: one conversion per two codes) by four warps, and P is f16.
 // The scales stay outside the products:
 //   z = S * (scale log2(e) 2^e k_scale) + log2(v_scale)          e: the query row's own power of two
