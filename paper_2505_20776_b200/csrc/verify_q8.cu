@@ -22,7 +22,7 @@
 //
 // What bounds it: the chain of a tile, not memory.  256 rows on a pair take 0.96 us a tile (128 keys: products 0.55, as much for the
 // exponentials), 128 rows on a CTA 0.95, on top of 12.5 us of launch, queries, last tile, stores and merge: 60 nodes of 32 query / 8
-// KV heads 27.0 us at 16K (1.2 TB/s of codes), 32 KV heads 28.1 at 8K (2.4).
+// KV heads 27.0 us at 16K (1.2 TB/s of codes), 32 KV heads 28.4 at 8K (2.4).
 #include "core.cuh"
 #include "q8.cuh"
 #include "tmap.h"
